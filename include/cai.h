@@ -435,6 +435,90 @@ int cai_head_rows_static(const void* W, int32_t V, int32_t H, const void* rows, 
  */
 int cai_test_static_wait_timeout(void);
 
+/*
+ * Operators on rows of vocabulary logits.  The paper decodes at temperature 0
+ * from logits that never reach memory; these four calls are for the programs
+ * around that: drawing tokens at a temperature, recording a teacher's largest
+ * logits, and training a student on such records.  They need no context and
+ * no workspace, allocate nothing, launch one kernel each and are asynchronous
+ * on `stream`; calls on different streams do not affect each other.
+ *
+ * logits: [M, V] device rows of `dtype` (CAI_BF16 or CAI_F32), ld >= V elements
+ * apart, aligned to their element size only.  M >= 0 (0: nothing is launched),
+ * 1 <= V <= 262144.  -inf and the type's lowest value mark tokens a row may not
+ * take.  Errors of all four: CAI_ERR_ARG (a null, misaligned or host pointer, a
+ * bad dtype, ld < V, a temperature that is not above 0 and finite),
+ * CAI_ERR_SHAPE (sizes), CAI_ERR_UNSUPPORTED, CAI_ERR_CUDA; nothing is launched
+ * then.
+ */
+#define CAI_BF16 0
+#define CAI_F32 1
+
+/*
+ * Draws one token from every row.  temperature, top_k, top_p, min_p: device
+ * arrays of M entries, or NULL for 1, off, off, off; u: M uniform numbers in
+ * [0, 1) (others are clamped into it, NaN is 0).  Per row, with T its temperature:
+ *   e_i = 2^((z_i - max z) (log2(e) / T)) in fp32, each operation rounded once,
+ *   w_i = e_i in units of 2^-40, rounded to the nearest whole number;
+ *   tokens are ordered by falling z, ties by rising index (-0 equals +0);
+ *   top_k in [1, V) keeps the first top_k tokens (else off), min_p keeps those
+ *   with e_i >= min(min_p, 1), and top_p < 1 then keeps of what is left the
+ *   shortest run from the front whose w reaches top_p of its whole (one token
+ *   at least);
+ *   token: the lowest index at which the kept w, added up in index order,
+ *   exceeds u times their whole; prob: its w over that whole.
+ * Sums of w are exact, so the result does not depend on how the row is split.
+ * T <= 0 (or NaN): the argmax (lowest index on ties) and its softmax
+ * probability at temperature 1, the filters aside.  A row without a softmax (a
+ * NaN or +inf logit, or none above -inf) gets prob NaN and a token below V: the
+ * first +inf where the maximum is +inf, else 0.
+ */
+int cai_sample_rows(const void* logits, int32_t dtype, int64_t ld, int32_t M, int32_t V,
+                    const float* temperature, const int32_t* top_k, const float* top_p,
+                    const float* min_p, const float* u, int32_t* token, float* prob, void* stream);
+
+/*
+ * Records every row's K largest logits: values [M, K] float and index [M, K],
+ * by falling value, ties by rising index, NaN above +inf; and lse [M], the
+ * log-sum-exp of the whole row at `temperature` (log sum_v exp(z_v / T)); NaN,
+ * +inf or -inf where the row's maximum is that.  1 <= K <= min(V, 512).
+ */
+int cai_top_rows(const void* logits, int32_t dtype, int64_t ld, int32_t M, int32_t V, int32_t K,
+                 double temperature, float* values, int32_t* index, float* lse, void* stream);
+
+/*
+ * The distillation loss of student rows against a teacher's record, and its
+ * gradient.  top_values, top_index [M, K]: the teacher's logits and their
+ * tokens (entries whose index is outside [0, V) are none; entries naming a
+ * token twice add up); 1 <= K <= 512.  With q the teacher's probabilities at
+ * `temperature` T and p = softmax(z / T):
+ *   top_lse == NULL: q = softmax(top_values / T) over the row's entries, q_r = 0;
+ *   else q_k = exp(top_values_k / T - top_lse) and q_r = max(0, 1 - sum q) is
+ *   the probability of all other tokens as one class (p_r in the student);
+ *   loss = weight T^2 [sum_k q_k (log q_k - log p_k) + q_r (log q_r - log p_r)].
+ * weight: [M] or NULL (1).  stats [M, 2]: the log-sum-exp of z / T over the row
+ * and over the tokens outside the record, for the backward call.  A row with
+ * weight 0, or without entries, is not read: loss, stats and gradient 0.
+ * grad (NULL: none): dloss/dz of every row, [M, V] of `dtype`, ld_grad apart;
+ * it may be the logits' own buffer with ld_grad = ld.  Where no token outside
+ * the record has any probability, those tokens' gradient is that of p alone.
+ */
+int cai_distill_loss(const void* logits, int32_t dtype, int64_t ld, int32_t M, int32_t V,
+                     int32_t K, const float* top_values, const int32_t* top_index,
+                     const float* top_lse, double temperature, const float* weight, float* loss,
+                     float* stats, void* grad, int64_t ld_grad, void* stream);
+
+/*
+ * The gradient alone: grad = grad_loss (device [M], the derivative by each
+ * row's loss) times dloss/dz, from the stats of cai_distill_loss for the same
+ * logits, record, weight and temperature.
+ */
+int cai_distill_backward(const void* logits, int32_t dtype, int64_t ld, int32_t M, int32_t V,
+                         int32_t K, const float* top_values, const int32_t* top_index,
+                         const float* top_lse, double temperature, const float* weight,
+                         const float* stats, const float* grad_loss, void* grad, int64_t ld_grad,
+                         void* stream);
+
 /* Static string for a status code. */
 const char* cai_strerror(int status);
 

@@ -43,6 +43,8 @@ CAI_DIAGNOSTICS = 128
 CAI_PRESET_LLADA = 0
 CAI_PRESET_DREAM = 1
 
+CAI_BF16, CAI_F32 = 0, 1
+
 CAI_MASK_TOKEN = -1
 CAI_RUNNING, CAI_EXIT_DONE, CAI_EXIT_GRIND, CAI_EXIT_TMAX = 0, 1, 2, 3
 
@@ -56,7 +58,8 @@ EXPORTS = ("cai_config_default", "cai_init", "cai_init_rmsnorm", "cai_first_step
            "cai_test_check_guards",
            "cai_head_rows_static", "cai_test_static_wait_timeout",
            "cai_init_vocab_shard", "cai_shard_rows", "cai_shard_head", "cai_shard_commit",
-           "cai_device_error_bits", "cai_pair_swap_limit")
+           "cai_device_error_bits", "cai_pair_swap_limit",
+           "cai_sample_rows", "cai_top_rows", "cai_distill_loss", "cai_distill_backward")
 
 
 class CaiError(RuntimeError):
@@ -104,7 +107,7 @@ def _load():
     if not os.path.exists(LIB_PATH):
         raise ImportError(f"libcai.so is not built ({LIB_PATH}); run paper_2608_22646_gb300.build")
     lib = ctypes.CDLL(LIB_PATH)
-    vp, i32 = ctypes.c_void_p, ctypes.c_int32
+    vp, i32, i64, f64 = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_double
     sig = {
         "cai_config_default": (ctypes.c_int, [ctypes.POINTER(cai_config), i32, i32, i32, i32, i32, i32, i32]),
         "cai_init": (ctypes.c_int, [ctypes.POINTER(cai_config), vp, vp, ctypes.POINTER(vp)]),
@@ -139,6 +142,12 @@ def _load():
         "cai_shard_rows": (ctypes.c_int, [vp, ctypes.POINTER(i32)]),
         "cai_shard_head": (ctypes.c_int, [vp, vp, vp, vp]),
         "cai_shard_commit": (ctypes.c_int, [vp, vp, i32, vp]),
+        "cai_sample_rows": (ctypes.c_int, [vp, i32, i64, i32, i32] + [vp] * 8),
+        "cai_top_rows": (ctypes.c_int, [vp, i32, i64, i32, i32, i32, f64, vp, vp, vp, vp]),
+        "cai_distill_loss": (ctypes.c_int, [vp, i32, i64, i32, i32, i32, vp, vp, vp, f64, vp, vp, vp,
+                                            vp, i64, vp]),
+        "cai_distill_backward": (ctypes.c_int, [vp, i32, i64, i32, i32, i32, vp, vp, vp, f64, vp, vp,
+                                                vp, vp, i64, vp]),
     }
     for name, (res, args) in sig.items():
         f = getattr(lib, name)
@@ -475,6 +484,108 @@ def cai_head_rows_static(W, rows, conf, argmax, stream=None) -> None:
 def cai_test_static_wait_timeout() -> None:
     """Make the next cai_head_rows_static call record a failed bounded wait."""
     _check(lib().cai_test_static_wait_timeout(), "cai_test_static_wait_timeout")
+
+
+# ------------------------------------------------ operators on rows of logits --
+
+def _rows(x, what: str) -> tuple[int, int, int, int, int]:
+    """(address, dtype code, row stride, M, V) of a 2-D device tensor of rows
+    whose elements are adjacent; rows may be any stride of at least V apart."""
+    full = str(x.dtype)
+    code = CAI_BF16 if full == "torch.bfloat16" else CAI_F32 if full == "torch.float32" else None
+    if code is None or x.ndim != 2 or not x.is_cuda:
+        raise ValueError(f"{what}: expected a 2-D torch.bfloat16 or torch.float32 CUDA tensor "
+                         f"(got {x.dtype}, shape {tuple(x.shape)}, on {x.device})")
+    (M, V), (ld, inner) = x.shape, x.stride()
+    if M <= 1:
+        ld = max(ld, V)
+    if (inner != 1 and V > 1) or ld < V:
+        raise ValueError(f"{what}: rows must be dense and at least V apart "
+                         f"(shape {tuple(x.shape)}, strides {x.stride()})")
+    return x.data_ptr(), code, ld, M, V
+
+
+def _arr(x, what: str, dtype: str, shape: tuple) -> int | None:
+    """Address of a contiguous device tensor of that element type and shape
+    (None stays None)."""
+    if x is None:
+        return None
+    if tuple(x.shape) != shape or not getattr(x, "is_cuda", False):
+        raise ValueError(f"{what}: expected a CUDA tensor of shape {shape}, got "
+                         f"{tuple(x.shape)} on {getattr(x, 'device', 'the host')}")
+    return _buf(x, what, dtype)
+
+
+def cai_sample_rows(logits, u, token, prob, temperature=None, top_k=None, top_p=None, min_p=None,
+                    stream=None) -> None:
+    """Draws a token from every row of ``logits`` [M, V] (bf16 or float32) with
+    the uniform numbers ``u`` [M]: its index into ``token`` (int32 [M]), its
+    probability among the tokens kept into ``prob`` (float32 [M]).  Settings
+    are float32 (``top_k``: int32) tensors [M], or None for 1 / off."""
+    ptr, code, ld, M, V = _rows(logits, "logits")
+    n = (M,)
+    _check(lib().cai_sample_rows(
+        ptr, code, ld, M, V, _arr(temperature, "temperature", "float32", n),
+        _arr(top_k, "top_k", "int32", n), _arr(top_p, "top_p", "float32", n),
+        _arr(min_p, "min_p", "float32", n), _arr(u, "u", "float32", n),
+        _arr(token, "token", "int32", n), _arr(prob, "prob", "float32", n), _stream(stream)),
+        "cai_sample_rows")
+
+
+def cai_top_rows(logits, values, index, lse, temperature: float = 1.0, stream=None) -> None:
+    """The K largest logits of every row, by falling value, into ``values``
+    (float32 [M, K]) and ``index`` (int32 [M, K]), and the row's log-sum-exp at
+    ``temperature`` into ``lse`` (float32 [M])."""
+    ptr, code, ld, M, V = _rows(logits, "logits")
+    K = int(values.shape[-1])
+    _check(lib().cai_top_rows(
+        ptr, code, ld, M, V, K, float(temperature), _arr(values, "values", "float32", (M, K)),
+        _arr(index, "index", "int32", (M, K)), _arr(lse, "lse", "float32", (M,)),
+        _stream(stream)), "cai_top_rows")
+
+
+def _record(logits, top_values, top_index, top_lse, temperature, weight):
+    ptr, code, ld, M, V = _rows(logits, "logits")
+    K = int(top_values.shape[-1])
+    return (M, V), code, (
+        ptr, code, ld, M, V, K, _arr(top_values, "top_values", "float32", (M, K)),
+        _arr(top_index, "top_index", "int32", (M, K)), _arr(top_lse, "top_lse", "float32", (M,)),
+        float(temperature), _arr(weight, "weight", "float32", (M,)))
+
+
+def _grad_rows(grad, shape, code) -> tuple[int | None, int]:
+    if grad is None:
+        return None, 0
+    ptr, gcode, ld, M, V = _rows(grad, "grad")
+    if (M, V) != shape or gcode != code:
+        raise ValueError(f"grad: expected the logits' shape {shape} and dtype, got {(M, V)} {grad.dtype}")
+    return ptr, ld
+
+
+def cai_distill_loss(logits, top_values, top_index, loss, stats, top_lse=None,
+                     temperature: float = 1.0, weight=None, grad=None, stream=None) -> None:
+    """Distillation loss of every row of ``logits`` [M, V] against the teacher's
+    record ``top_values`` / ``top_index`` [M, K] into ``loss`` (float32 [M]),
+    the statistics for the backward call into ``stats`` (float32 [M, 2]) and,
+    with ``grad`` (like logits, or the logits themselves), the gradient of each
+    row's loss.  ``top_lse`` [M]: the teacher's log-sum-exp at ``temperature``
+    (then the tokens outside the record count as one class)."""
+    shape, code, args = _record(logits, top_values, top_index, top_lse, temperature, weight)
+    gptr, gld = _grad_rows(grad, shape, code)
+    _check(lib().cai_distill_loss(*args, _arr(loss, "loss", "float32", shape[:1]),
+                                  _arr(stats, "stats", "float32", (shape[0], 2)), gptr, gld,
+                                  _stream(stream)), "cai_distill_loss")
+
+
+def cai_distill_backward(logits, top_values, top_index, stats, grad_loss, grad, top_lse=None,
+                         temperature: float = 1.0, weight=None, stream=None) -> None:
+    """``grad`` = ``grad_loss`` [M] times the gradient of each row's distillation
+    loss, from the ``stats`` of cai_distill_loss on the same arguments."""
+    shape, code, args = _record(logits, top_values, top_index, top_lse, temperature, weight)
+    gptr, gld = _grad_rows(grad, shape, code)
+    _check(lib().cai_distill_backward(*args, _arr(stats, "stats", "float32", (shape[0], 2)),
+                                      _arr(grad_loss, "grad_loss", "float32", shape[:1]), gptr, gld,
+                                      _stream(stream)), "cai_distill_backward")
 
 
 def config_from_dict(d: dict) -> cai_config:

@@ -11,9 +11,9 @@ CSRC = os.path.join(PKG, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(PKG, "libcai.so")
 LIB_DEBUG = os.path.join(PKG, "libcai_debug.so")  # CAI_DEBUG: range checks on index lists
-SOURCES = ["cai.cu"]
-DEPS = ["cai.cu", "ptx.cuh", "softmax.cuh", "commit.cuh", "head_kernel.cuh", "step_kernels.cuh", "pair_kernel.cuh",
-        "rows_kernel.cuh", "static_head.cuh"]
+SOURCES = ["cai.cu", "logit_ops.cu"]
+DEPS = SOURCES + ["ptx.cuh", "softmax.cuh", "commit.cuh", "head_kernel.cuh", "step_kernels.cuh", "pair_kernel.cuh",
+                  "rows_kernel.cuh", "static_head.cuh", "row_ops.cuh", "sample.cuh", "distill.cuh"]
 
 
 def _stale(lib: str = LIB) -> bool:
@@ -32,13 +32,25 @@ def build(force: bool = False, verbose: bool = False, debug: bool = False) -> st
     nvcc = os.environ.get("NVCC", "nvcc")
     tmp = lib + f".tmp{os.getpid()}"
     cmd = [nvcc, "-gencode", "arch=compute_103a,code=sm_103a", "-O3", "-lineinfo", "-std=c++17",
-           "-Xcompiler", "-fPIC", "-shared", "-I", INCLUDE, "-o", tmp]
+           "-Xcompiler", "-fPIC", "-I", INCLUDE]
     if debug:
         cmd += ["-DCAI_DEBUG"]
     if verbose:
         cmd += ["-Xptxas", "-v"]
-    cmd += [os.path.join(CSRC, s) for s in SOURCES]
-    subprocess.check_call(cmd, stdout=None if verbose else subprocess.DEVNULL)
+    out = None if verbose else subprocess.DEVNULL
+    objs = [f"{tmp}.{s}.o" for s in SOURCES]
+    try:
+        jobs = [subprocess.Popen(cmd + ["-c", "-o", o, os.path.join(CSRC, s)], stdout=out)
+                for s, o in zip(SOURCES, objs)]
+        for s, job in zip(SOURCES, [j.wait() for j in jobs]):  # every one has ended
+            if job != 0:
+                raise subprocess.CalledProcessError(job, f"nvcc {s}")
+        subprocess.check_call([nvcc, "-shared", "-gencode", "arch=compute_103a,code=sm_103a", "-o", tmp] + objs,
+                              stdout=out)
+    finally:
+        for o in objs:
+            if os.path.exists(o):
+                os.remove(o)
     os.replace(tmp, lib)
     return lib
 
