@@ -519,6 +519,45 @@ int cai_distill_backward(const void* logits, int32_t dtype, int64_t ld, int32_t 
                          const float* stats, const float* grad_loss, void* grad, int64_t ld_grad,
                          void* stream);
 
+/*
+ * An LM-head weight in microscaled 4-bit floating point.  The paper has no
+ * counterpart: a step of few rows is bound by the weight's bytes, 2 V H in bf16
+ * and 17/32 V H here.  Blocks of 32 values along H share a power of two (E8M0);
+ * the values are E2M1.  For a block with largest magnitude a the scale is
+ * 2^(floor(log2 a) - 2), at least 2^-127 (a = 0: all codes 0); x / scale goes to
+ * the nearest of 0, 0.5, 1, 1.5, 2, 3, 4, 6, ties to the even code, larger ones
+ * to 6.  A block with a NaN or an infinity has no scale: it stands for NaNs.
+ *
+ * cai_mx4_init quantises W [V, H] (device, row-major, CAI_BF16 or CAI_F32,
+ * 16-byte aligned; read during this call) into a handle on the current device,
+ * with room for max_rows rows a call.  1 <= V <= 2^22, H % 64 == 0, 64 <= H <=
+ * 16384, 1 <= max_rows <= 65536 (else CAI_ERR_SHAPE).  Synchronous.  The weight
+ * takes 17/32 V H bytes and some padding.
+ * cai_mx4_update quantises W anew (same sizes), asynchronously on `stream`;
+ * with `values` (bf16 [V, H], 16-byte aligned, may not overlap W) it also
+ * writes what the codes stand for, exactly: the weight that a training step's
+ * forward pass sees.
+ * cai_mx4_logits quantises rows [M, H] the same way (0 <= M <= max_rows,
+ * 16-byte aligned) and writes their products with the weight, out [M, V] of
+ * out_dtype, ld >= V apart, aligned to its element size: fp32 sums of exact
+ * products, rounded once.  Two launches, asynchronous on `stream`.
+ * The handle keeps the call's quantised rows: calls on one handle belong on one
+ * stream, or are ordered by events.  Not thread safe.
+ * Errors: CAI_ERR_ARG (null, misaligned or host pointers, a bad dtype, ld < V,
+ * another device current), CAI_ERR_SHAPE, CAI_ERR_UNSUPPORTED, CAI_ERR_NOMEM,
+ * CAI_ERR_CUDA, and CAI_ERR_DEVICE once a bounded wait of the handle's kernels
+ * gave up (cai_mx4_error_bits tells which; that call's outputs are not valid).
+ * cai_mx4_free synchronises the device; NULL is a no-op.
+ */
+typedef struct cai_mx4 cai_mx4;
+int cai_mx4_init(const void* W, int32_t dtype, int32_t V, int32_t H, int32_t max_rows,
+                 void* stream, cai_mx4** out);
+int cai_mx4_update(cai_mx4* head, const void* W, int32_t dtype, void* values, void* stream);
+int cai_mx4_logits(cai_mx4* head, const void* rows, int32_t dtype, int32_t M, void* out,
+                   int32_t out_dtype, int64_t ld, void* stream);
+int cai_mx4_error_bits(const cai_mx4* head, uint32_t* bits);
+void cai_mx4_free(cai_mx4* head);
+
 /* Static string for a status code. */
 const char* cai_strerror(int status);
 

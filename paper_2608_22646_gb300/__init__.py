@@ -59,7 +59,8 @@ EXPORTS = ("cai_config_default", "cai_init", "cai_init_rmsnorm", "cai_first_step
            "cai_head_rows_static", "cai_test_static_wait_timeout",
            "cai_init_vocab_shard", "cai_shard_rows", "cai_shard_head", "cai_shard_commit",
            "cai_device_error_bits", "cai_pair_swap_limit",
-           "cai_sample_rows", "cai_top_rows", "cai_distill_loss", "cai_distill_backward")
+           "cai_sample_rows", "cai_top_rows", "cai_distill_loss", "cai_distill_backward",
+           "cai_mx4_init", "cai_mx4_update", "cai_mx4_logits", "cai_mx4_error_bits", "cai_mx4_free")
 
 
 class CaiError(RuntimeError):
@@ -146,6 +147,11 @@ def _load():
         "cai_top_rows": (ctypes.c_int, [vp, i32, i64, i32, i32, i32, f64, vp, vp, vp, vp]),
         "cai_distill_loss": (ctypes.c_int, [vp, i32, i64, i32, i32, i32, vp, vp, vp, f64, vp, vp, vp,
                                             vp, i64, vp]),
+        "cai_mx4_init": (ctypes.c_int, [vp, i32, i32, i32, i32, vp, ctypes.POINTER(vp)]),
+        "cai_mx4_update": (ctypes.c_int, [vp, vp, i32, vp, vp]),
+        "cai_mx4_logits": (ctypes.c_int, [vp, vp, i32, i32, vp, i32, i64, vp]),
+        "cai_mx4_error_bits": (ctypes.c_int, [vp, ctypes.POINTER(ctypes.c_uint32)]),
+        "cai_mx4_free": (None, [vp]),
         "cai_distill_backward": (ctypes.c_int, [vp, i32, i64, i32, i32, i32, vp, vp, vp, f64, vp, vp,
                                                 vp, vp, i64, vp]),
     }
@@ -586,6 +592,74 @@ def cai_distill_backward(logits, top_values, top_index, stats, grad_loss, grad, 
     _check(lib().cai_distill_backward(*args, _arr(stats, "stats", "float32", (shape[0], 2)),
                                       _arr(grad_loss, "grad_loss", "float32", shape[:1]), gptr, gld,
                                       _stream(stream)), "cai_distill_backward")
+
+
+# ------------------------------------------------------------ the 4-bit LM head --
+
+class Mx4:
+    """Owning handle of a ``cai_mx4*``; ``with cai_mx4_init(W, n) as head:``
+    frees it on exit."""
+
+    def __init__(self, handle: int, V: int, H: int, max_rows: int):
+        self.handle, self.V, self.H, self.max_rows = handle, V, H, max_rows
+
+    def __enter__(self) -> "Mx4":
+        return self
+
+    def __exit__(self, *exc) -> None:
+        cai_mx4_free(self)
+
+
+def _dense(x, what: str) -> tuple[int, int, int, int]:
+    """(address, dtype code, rows, columns) of a contiguous 2-D device tensor."""
+    ptr, code, ld, M, N = _rows(x, what)
+    if ld != N:
+        raise ValueError(f"{what}: expected a contiguous tensor (strides {x.stride()})")
+    return ptr, code, M, N
+
+
+def cai_mx4_init(W, max_rows: int, stream=None) -> Mx4:
+    """Quantises the LM-head weight ``W`` [V, H] (bf16 or float32 CUDA tensor)
+    to microscaled 4-bit floating point; at most ``max_rows`` rows a call."""
+    ptr, code, V, H = _dense(W, "W")
+    h = ctypes.c_void_p()
+    _check(lib().cai_mx4_init(ptr, code, V, H, int(max_rows), _stream(stream), ctypes.byref(h)),
+           "cai_mx4_init")
+    return Mx4(h.value, V, H, int(max_rows))
+
+
+def cai_mx4_update(head: Mx4, W, values=None, stream=None) -> None:
+    """Quantises ``W`` anew into ``head``; ``values`` (bf16 [V, H]) receives
+    what the codes stand for."""
+    ptr, code, V, H = _dense(W, "W")
+    if (V, H) != (head.V, head.H):
+        raise ValueError(f"W: expected shape {(head.V, head.H)}, got {(V, H)}")
+    _check(lib().cai_mx4_update(head.handle, ptr, code, _arr(values, "values", "bfloat16", (V, H)),
+                                _stream(stream)), "cai_mx4_update")
+
+
+def cai_mx4_logits(head: Mx4, rows, out, stream=None) -> None:
+    """``out`` [M, V] (bf16 or float32, rows any stride of at least V apart) =
+    quantised ``rows`` [M, H] (bf16 or float32) times the quantised weight."""
+    ptr, code, M, H = _dense(rows, "rows")
+    optr, ocode, ld, Mo, V = _rows(out, "out")
+    if H != head.H or (Mo, V) != (M, head.V):
+        raise ValueError(f"rows {(M, H)} and out {(Mo, V)} do not fit a head of V = {head.V}, H = {head.H}")
+    _check(lib().cai_mx4_logits(head.handle, ptr, code, M, optr, ocode, ld, _stream(stream)),
+           "cai_mx4_logits")
+
+
+def cai_mx4_error_bits(head: Mx4) -> int:
+    """Bits of the waits that gave up in the head's kernels (DEVERR_NAMES)."""
+    v = ctypes.c_uint32(0)
+    _check(lib().cai_mx4_error_bits(head.handle, ctypes.byref(v)), "cai_mx4_error_bits")
+    return int(v.value)
+
+
+def cai_mx4_free(head: Mx4) -> None:
+    if head.handle:
+        lib().cai_mx4_free(head.handle)
+        head.handle = 0
 
 
 def config_from_dict(d: dict) -> cai_config:

@@ -11,9 +11,10 @@ CSRC = os.path.join(PKG, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(PKG, "libcai.so")
 LIB_DEBUG = os.path.join(PKG, "libcai_debug.so")  # CAI_DEBUG: range checks on index lists
-SOURCES = ["cai.cu", "logit_ops.cu"]
+SOURCES = ["cai.cu", "logit_ops.cu", "mx4.cu"]
 DEPS = SOURCES + ["ptx.cuh", "softmax.cuh", "commit.cuh", "head_kernel.cuh", "step_kernels.cuh", "pair_kernel.cuh",
-                  "rows_kernel.cuh", "static_head.cuh", "row_ops.cuh", "sample.cuh", "distill.cuh"]
+                  "rows_kernel.cuh", "static_head.cuh", "row_ops.cuh", "sample.cuh", "distill.cuh",
+                  "mx4.cuh", "internal.h"]
 
 
 def _stale(lib: str = LIB) -> bool:

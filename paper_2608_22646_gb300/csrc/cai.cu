@@ -19,6 +19,7 @@
 #include <vector>
 
 #include "cai.h"
+#include "internal.h"
 #include "pair_kernel.cuh"
 #include "rows_kernel.cuh"
 #include "step_kernels.cuh"
@@ -116,6 +117,12 @@ int dev_alloc(void** p, size_t bytes) {
   if (e != cudaSuccess) return CAI_ERR_CUDA;
   return CAI_OK;
 }
+
+}  // namespace
+
+int cai::device_alloc(void** p, size_t bytes) { return dev_alloc(p, bytes); }
+
+namespace {
 
 typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*,
                                   const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
