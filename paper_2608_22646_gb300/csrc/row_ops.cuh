@@ -69,6 +69,28 @@ struct Row<__nv_bfloat16> {
   }
 };
 
+// max that keeps a NaN.
+__device__ __forceinline__ float max_nan(float a, float b) {
+  float r;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+  return r;
+}
+
+// The largest of a vector and of `m`, NaN kept.
+__device__ __forceinline__ float vec_max(const uint4& v, float m, float) {
+  m = max_nan(m, max_nan(__uint_as_float(v.x), __uint_as_float(v.y)));
+  return max_nan(m, max_nan(__uint_as_float(v.z), __uint_as_float(v.w)));
+}
+__device__ __forceinline__ uint32_t max2_nan(uint32_t a, uint32_t b) {
+  uint32_t r;
+  asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  return r;
+}
+__device__ __forceinline__ float vec_max(const uint4& v, float m, __nv_bfloat16) {
+  const uint32_t r = max2_nan(max2_nan(v.x, v.y), max2_nan(v.z, v.w));
+  return max_nan(m, max_nan(__uint_as_float(r << 16), __uint_as_float(r & 0xffff0000u)));
+}
+
 // Order of the logits as whole numbers: rises with the value, -0 and +0 are the
 // same, NaN is above +inf.  bf16 values differ in the upper 16 bits alone.
 template <typename T>
@@ -82,13 +104,6 @@ template <typename T>
 __device__ __forceinline__ float value_of_key(uint32_t k) {
   if (Row<T>::kKeyBits == 16) k = (k << 16) | (k & 0x8000u ? 0u : 0xffffu);
   return __uint_as_float(k & 0x80000000u ? k ^ 0x80000000u : ~k);
-}
-
-// max that keeps a NaN.
-__device__ __forceinline__ float max_nan(float a, float b) {
-  float r;
-  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
-  return r;
 }
 
 // The slice of a row that this CTA keeps: elements [lo, hi) of the row, element
@@ -192,19 +207,27 @@ struct Tally {  // tokens and their weight
 };
 
 constexpr int kBins = 1024;
+constexpr int kListMax = 2048;  // candidates that one CTA finishes alone
+constexpr int kSums = 3;        // values of an exchange
 
 // Shared memory of a CTA beside its slice.
 struct RowShared {
-  unsigned long long wred[kRowMaxWarps];       // one value per warp
-  unsigned long long slots[4][kRowMaxCluster]; // one value per CTA, written by the peers
+  unsigned long long wred[kSums][kRowMaxWarps];          // values per warp
+  unsigned long long slots[4][kSums][kRowMaxCluster];    // values per CTA, written by the peers
   Tally parts[kRowMaxCluster];
   Tally found, found_at;  // what lies above the bin that was found, and in it
   uint32_t found_bin;
   int32_t told;           // an index one thread found, for all (tell_index)
   unsigned long long part_scan[kRowMaxWarps];
   uint32_t part_scan_n[kRowMaxWarps];
-  unsigned long long mass[kBins];
-  uint32_t count[kBins];
+  uint32_t listed;        // candidates pushed so far (in CTA 0)
+  union {
+    struct {              // find_cut
+      unsigned long long mass[kBins];
+      uint32_t count[kBins];
+    };
+    unsigned long long list[kListMax];  // candidates (in CTA 0)
+  };
 };
 
 struct RowCta {
@@ -258,34 +281,49 @@ __device__ __forceinline__ unsigned long long warp_reduce(unsigned long long v, 
 }
 
 // Reduces one value per thread over the CTA, the result in every thread.  All
-// threads call it; wred may be used again after the next __syncthreads.
+// threads call it; wred is free again after the next barrier.
 template <typename Op>
 __device__ __forceinline__ unsigned long long cta_reduce(const RowCta& c, unsigned long long v,
-                                                         Op op) {
+                                                         Op op, int which = 0) {
   v = warp_reduce(v, op);
   const int warp = threadIdx.x >> 5, n = blockDim.x >> 5;
-  if ((threadIdx.x & 31) == 0) c.sh->wred[warp] = v;
+  if ((threadIdx.x & 31) == 0) c.sh->wred[which][warp] = v;
   __syncthreads();
-  unsigned long long r = c.sh->wred[0];
-  for (int i = 1; i < n; ++i) r = op(r, c.sh->wred[i]);
+  unsigned long long r = c.sh->wred[which][0];
+  for (int i = 1; i < n; ++i) r = op(r, c.sh->wred[which][i]);
   return r;
 }
 
-// One value per CTA to every CTA of the cluster, in rank order in the returned
-// slots.  They stay valid for the next three exchanges.
-__device__ __forceinline__ const unsigned long long* cluster_exchange(RowCta& c,
-                                                                      unsigned long long v) {
-  unsigned long long* s = c.sh->slots[c.turn & 3];
+// Values per CTA to every CTA of the cluster: the slots of value `which`, in rank
+// order, are valid for the next three exchanges.
+struct Parts {
+  const unsigned long long* slot;
+  __device__ __forceinline__ const unsigned long long* of(int which) const {
+    return slot + which * kRowMaxCluster;
+  }
+  __device__ __forceinline__ unsigned long long sum(int ctas, int which) const {
+    unsigned long long r = 0;
+    for (int i = 0; i < ctas; ++i) r += of(which)[i];
+    return r;
+  }
+};
+template <int kN>
+__device__ __forceinline__ Parts cluster_exchange(RowCta& c, const unsigned long long (&v)[kN]) {
+  unsigned long long* s = &c.sh->slots[c.turn & 3][0][0];
   c.turn++;
-  if (static_cast<int>(threadIdx.x) < c.ctas) st_peer(s + c.rank, threadIdx.x, v);
+  if (static_cast<int>(threadIdx.x) < c.ctas) {
+#pragma unroll
+    for (int i = 0; i < kN; ++i) st_peer(s + i * kRowMaxCluster + c.rank, threadIdx.x, v[i]);
+  }
   row_sync();
-  return s;
+  return Parts{s};
 }
 
 template <typename Op>
 __device__ __forceinline__ unsigned long long cluster_reduce(RowCta& c, unsigned long long v,
                                                              Op op) {
-  const unsigned long long* s = cluster_exchange(c, cta_reduce(c, v, op));
+  const unsigned long long mine[1] = {cta_reduce(c, v, op)};
+  const unsigned long long* s = cluster_exchange(c, mine).of(0);
   unsigned long long r = s[0];
   for (int i = 1; i < c.ctas; ++i) r = op(r, s[i]);
   return r;
@@ -295,6 +333,30 @@ struct AddOp {
   __device__ __forceinline__ unsigned long long operator()(unsigned long long a,
                                                            unsigned long long b) const {
     return a + b;
+  }
+};
+// The sums of up to three values per thread, CTA by CTA, to all.
+template <int kN>
+__device__ __forceinline__ Parts exchange_sums(RowCta& c, const unsigned long long (&v)[kN]) {
+  const int warp = threadIdx.x >> 5, n = blockDim.x >> 5;
+  unsigned long long r[kN];
+#pragma unroll
+  for (int i = 0; i < kN; ++i) {
+    r[i] = warp_reduce(v[i], AddOp());
+    if ((threadIdx.x & 31) == 0) c.sh->wred[i][warp] = r[i];
+  }
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < kN; ++i) {
+    r[i] = 0;
+    for (int w = 0; w < n; ++w) r[i] += c.sh->wred[i][w];
+  }
+  return cluster_exchange(c, r);
+}
+struct MaxOp {
+  __device__ __forceinline__ unsigned long long operator()(unsigned long long a,
+                                                           unsigned long long b) const {
+    return a > b ? a : b;
   }
 };
 struct MaxNanOp {  // on the bits of a float
@@ -457,9 +519,9 @@ __device__ __forceinline__ int find_index(const RowCta& c, const Slice<T>& s,
     if ((tid & 31) >= o) incl += m;
   }
   __syncthreads();  // wred is free
-  if ((tid & 31) == 31) c.sh->wred[tid >> 5] = incl;
+  if ((tid & 31) == 31) c.sh->wred[0][tid >> 5] = incl;
   __syncthreads();
-  for (int w = 0; w < (tid >> 5); ++w) incl += c.sh->wred[w];
+  for (int w = 0; w < (tid >> 5); ++w) incl += c.sh->wred[0][w];
   unsigned long long run = base + incl - own;
   if (drawn < run || drawn >= run + own) return -1;
   for (int i = a; i < b; ++i) {
@@ -478,6 +540,90 @@ __device__ __forceinline__ int tell_index(const RowCta& c, int found) {
   return c.sh->told;
 }
 
+// ------------------------------------------------------------- candidates --
+
+// A key with at least `count` elements of this CTA's slice at or above it, near
+// the largest such: the count-th largest of the threads' maxima (each stands for
+// an element), its lower 16 bits cleared in 32-bit keys.  0 where the CTA has
+// fewer threads than that.  All threads call it.
+template <typename T>
+__device__ __forceinline__ uint32_t local_floor(float thread_max, int count) {
+  constexpr int kDrop = Row<T>::kKeyBits - 16;
+  const uint32_t key = key_of<T>(thread_max) >> kDrop;
+  uint32_t found = 0;
+#pragma unroll 1
+  for (int bit = 15; bit >= 0; --bit) {
+    const uint32_t t = found | (1u << bit);
+    if (__syncthreads_count(key >= t) >= count) found = t;
+  }
+  return found << kDrop;
+}
+
+// Order of candidates: falling key, then rising index.
+__device__ __forceinline__ unsigned long long candidate(uint32_t key, int index) {
+  return (static_cast<unsigned long long>(~key) << 32) | static_cast<uint32_t>(index);
+}
+__device__ __forceinline__ uint32_t candidate_key(unsigned long long x) {
+  return ~static_cast<uint32_t>(x >> 32);
+}
+__device__ __forceinline__ int candidate_index(unsigned long long x) {
+  return static_cast<int>(static_cast<uint32_t>(x));
+}
+
+// Appends a candidate to CTA 0's list; past its end they are only counted.
+__device__ __forceinline__ void push_candidate(const RowCta& c, uint32_t key, int index) {
+  uint32_t at;
+  asm volatile("atom.relaxed.cluster.shared::cluster.add.u32 %0, [%1], 1;"
+               : "=r"(at)
+               : "r"(mapa_shared(&c.sh->listed, 0))
+               : "memory");
+  if (at < kListMax) st_peer(c.sh->list + at, 0, candidate(key, index));
+}
+
+// Sorts n (a power of two) 64-bit values in shared memory, rising.
+__device__ __forceinline__ void cta_sort(unsigned long long* a, int n) {
+  for (int k = 2; k <= n; k <<= 1)
+    for (int j = k >> 1; j > 0; j >>= 1) {
+      for (int q = threadIdx.x; q < n / 2; q += blockDim.x) {
+        const int i = ((q & ~(j - 1)) << 1) | (q & (j - 1));
+        const unsigned long long x = a[i], y = a[i + j];
+        if ((x > y) == ((i & k) == 0)) {
+          a[i] = y;
+          a[i + j] = x;
+        }
+      }
+      __syncthreads();
+    }
+}
+// ... n of any size, with room up to the next power of two.
+__device__ __forceinline__ void cta_sort_any(unsigned long long* a, int n) {
+  const int size = n > 1 ? 1 << (32 - __clz(n - 1)) : 1;
+  for (int i = n + threadIdx.x; i < size; i += blockDim.x) a[i] = ~0ull;
+  __syncthreads();
+  cta_sort(a, size);
+}
+
+// The sum of the values before this thread's, and of all.
+__device__ __forceinline__ unsigned long long cta_scan(const RowCta& c, unsigned long long v,
+                                                       unsigned long long& whole) {
+  unsigned long long incl = v;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const unsigned long long m = __shfl_up_sync(0xffffffffu, incl, o);
+    if ((threadIdx.x & 31) >= o) incl += m;
+  }
+  __syncthreads();
+  if ((threadIdx.x & 31) == 31) c.sh->wred[0][threadIdx.x >> 5] = incl;
+  __syncthreads();
+  unsigned long long before = incl - v;
+  whole = 0;
+  for (int w = 0; w < static_cast<int>(blockDim.x >> 5); ++w) {
+    if (w < static_cast<int>(threadIdx.x >> 5)) before += c.sh->wred[0][w];
+    whole += c.sh->wred[0][w];
+  }
+  return before;
+}
+
 // The cluster that reads a row: as few CTAs as keep a slice within
 // kSliceTarget, more while the grid leaves SMs idle and slices stay long.
 __host__ __forceinline__ int row_ctas(int M, int V, int elem, int sms) {
@@ -488,9 +634,9 @@ __host__ __forceinline__ int row_ctas(int M, int V, int elem, int sms) {
   return c;
 }
 
-// Threads of a CTA: about 16 elements for each, whole warps.
+// Threads of a CTA: about 8 elements for each, whole warps.
 __host__ __forceinline__ int row_threads(int V, int ctas) {
-  const int n = (row_chunk(V, ctas) + 15) / 16;
+  const int n = (row_chunk(V, ctas) + 7) / 8;
   return n < 128 ? 128 : n > kRowMaxThreads ? kRowMaxThreads : (n + 31) / 32 * 32;
 }
 
