@@ -8,9 +8,8 @@
 //   loss = w tau^2 [ sum_k q_k (log q_k - log p_k) + q_r (log q_r - log p_r) ]
 //   dloss/dz_v = w tau (A p_v - q_v)            in the record
 //              = w tau (A p_r - q_r) p_v / p_r  outside,   A = sum q + q_r.
-// p_r is summed over the tokens outside, never 1 minus the others: once the
-// slice is in shared memory the record's logits are taken out of it and -inf
-// left in their places, so the pass over the slice sees the rest alone.
+// p_r is summed over the tokens outside, never 1 minus the others: a bitmap of the
+// slice tells the pass over it which elements the record names.
 #pragma once
 
 #include "row_ops.cuh"
@@ -77,68 +76,113 @@ template <typename Op>
 __device__ __forceinline__ float cta_float(float* scratch, float v, Op op) {
 #pragma unroll
   for (int o = 16; o >= 1; o >>= 1) v = op(v, __shfl_xor_sync(0xffffffffu, v, o));
+  const int n = blockDim.x >> 5;  // a power of two
   __syncthreads();
   if ((threadIdx.x & 31) == 0) scratch[threadIdx.x >> 5] = v;
   __syncthreads();
-  float r = scratch[0];
-  for (int i = 1; i < static_cast<int>(blockDim.x >> 5); ++i) r = op(r, scratch[i]);
-  return r;
+  v = scratch[threadIdx.x & (n - 1)];
+#pragma unroll 1
+  for (int o = n >> 1; o >= 1; o >>= 1) v = op(v, __shfl_xor_sync(0xffffffffu, v, o));
+  return v;
 }
 
-// Marks in place of an element: an index below 2^16 as bits of the element's
-// type (never read as a value).
-__device__ __forceinline__ float mark_of(int k, float) { return __uint_as_float(k); }
-__device__ __forceinline__ __nv_bfloat16 mark_of(int k, __nv_bfloat16) {
-  return __ushort_as_bfloat16(static_cast<unsigned short>(k));
-}
-__device__ __forceinline__ int of_mark(float x) { return static_cast<int>(__float_as_uint(x)); }
-__device__ __forceinline__ int of_mark(__nv_bfloat16 x) { return __bfloat16_as_ushort(x); }
-
+// Bits of the slice's vectors, kVec for each: which elements the record names.
 template <typename T>
-__global__ void __launch_bounds__(kRowMaxThreads)
+__device__ __forceinline__ uint32_t vector_bits(const uint32_t* bits, int v) {
+  constexpr int kVec = Row<T>::kVec;
+  return (bits[v / (32 / kVec)] >> (v % (32 / kVec) * kVec)) & ((1u << kVec) - 1u);
+}
+__host__ __device__ __forceinline__ size_t bitmap_bytes(int slice_elems) {
+  return (static_cast<size_t>(slice_elems) + 16 + 31) / 32 * 4;
+}
+
+// Dynamic shared memory: the slice (kCluster), then the bitmap.
+template <typename T, bool kCluster>
+__global__ void __launch_bounds__(kCluster ? 512 : 1024, 1)
     distill_kernel(const __grid_constant__ DistillParams p, int ctas) {
   constexpr int kVec = Row<T>::kVec;
   extern __shared__ __align__(16) unsigned char slice_smem[];
   __shared__ RowShared sh;
   __shared__ Record rec;
-  row_begin();
-  RowCta c{&sh, static_cast<int>(cluster_ctarank()), ctas, 0};
-  const int r = blockIdx.x / ctas, tid = threadIdx.x, nt = blockDim.x;
+  using Cta = RowCta<kCluster>;
+  Cta::begin();
+  Cta c(&sh, ctas);
+  const int r = kCluster ? blockIdx.x / ctas : blockIdx.x, tid = threadIdx.x, nt = blockDim.x;
   const float inf = __uint_as_float(0x7f800000u);
   const T* row = static_cast<const T*>(p.logits) + static_cast<long long>(r) * p.ld;
   T* grow = static_cast<T*>(p.grad) + static_cast<long long>(r) * p.ld_grad;
-  const Slice<T> s = row_slice(row, p.V, c.rank, ctas, slice_smem);
+  const Slice<T, kCluster> s = row_slice<T, kCluster>(row, p.V, c.rank(), c.ctas(), slice_smem, sh.edge);
+  uint32_t* bits = reinterpret_cast<uint32_t*>(
+      slice_smem + (kCluster ? row_slice_bytes(p.V, c.ctas(), sizeof(T)) : 0));
   const bool backward = p.upstream != nullptr;
   const float w = p.weight ? p.weight[r] : 1.0f;
+  const uint32_t a_in = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(row + s.lo)) & 15u;
+  const uint32_t a_out = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(grow + s.lo)) & 15u;
+  uint4* dst = reinterpret_cast<uint4*>(reinterpret_cast<uintptr_t>(grow + s.lo) &
+                                        ~static_cast<uintptr_t>(15));
 
-  // The record: probabilities of its entries, the same in every CTA.
+  // The record: probabilities of its entries, the same in every CTA; the
+  // student's logits of those in this CTA's slice.
   float high = -inf;
-  for (int k = tid; k < p.K; k += nt) {
-    const int at = p.top_index[static_cast<long long>(r) * p.K + k];
-    const float t = __fdiv_rn(p.top_values[static_cast<long long>(r) * p.K + k], p.tau);
-    const bool given = at >= 0 && at < p.V;
-    rec.at[k] = given ? at : -1;
-    rec.logq[k] = given ? t : -inf;
-    if (given) high = fmaxf(high, t);
-  }
-  const auto max_op = [](float a, float b) { return fmaxf(a, b); };
-  const auto add_op = [](float a, float b) { return a + b; };
   bool any = false;
-  for (int k = tid; k < p.K; k += nt) any |= rec.at[k] >= 0;
-  const bool live = w != 0.0f && __syncthreads_or(any);
-  if (!live) {  // the same in the whole cluster; the row is not read
-    if (p.grad)
-      for (int i = s.lo + tid; i < s.hi; i += nt) grow[i] = Row<T>::from_float(0.0f);
-    if (c.rank == 0 && tid == 0 && p.loss) {
+  if (w != 0.0f)
+#pragma unroll 1
+    for (int k = tid; k < p.K; k += nt) {
+      const int at = p.top_index[static_cast<long long>(r) * p.K + k];
+      const float t = __fdiv_rn(p.top_values[static_cast<long long>(r) * p.K + k], p.tau);
+      const bool given = at >= 0 && at < p.V;
+      any |= given;
+      rec.at[k] = given ? at : -1;
+      rec.logq[k] = given ? t : -inf;
+      rec.z[k] = given && s.holds(at) ? Row<T>::to_float(row[at]) : 0.0f;
+      if (given) high = fmaxf(high, t);
+    }
+  const int n_bits = (s.n_vec * kVec + 31) / 32;
+#pragma unroll 1
+  for (int i = tid; i < n_bits; i += nt) bits[i] = 0;
+  if (!__syncthreads_or(any)) {  // the same in the whole cluster; the row is not read
+    if (p.grad) {
+      if (a_in == a_out) {
+#pragma unroll 1
+        for (int v = tid; v < s.n_vec; v += nt)
+          if (v >= s.first && v < s.last)
+            dst[v] = make_uint4(0u, 0u, 0u, 0u);
+          else
+#pragma unroll 1
+            for (int e = 0; e < kVec; ++e)
+              if (s.holds(s.index(v) + e)) grow[s.index(v) + e] = Row<T>::from_float(0.0f);
+      } else {
+#pragma unroll 1
+        for (int i = s.lo + tid; i < s.hi; i += nt) grow[i] = Row<T>::from_float(0.0f);
+      }
+    }
+    if (c.rank() == 0 && tid == 0 && p.loss) {
       p.loss[r] = 0.0f;
       p.stats[2ll * r] = 0.0f;
       p.stats[2ll * r + 1] = 0.0f;
     }
-    row_begun();
+    c.begun();
     return;
   }
-  load_slice<T, 4>(s, row, [](const uint4&) {});
-  row_begun();
+
+  // Mark the record's tokens.  The entry that finds its token unmarked speaks for
+  // it.
+  static_assert(kTopMax / 64 <= 32, "one bit for each entry of a thread");
+  uint32_t speaks = 0;  // bit j: entry tid + j nt speaks for its token
+  bool twice = false;
+#pragma unroll 1
+  for (int k = tid, j = 0; k < p.K; k += nt, ++j) {
+    const int at = rec.at[k];
+    if (at >= 0 && s.holds(at)) {
+      const uint32_t i = static_cast<uint32_t>(at - s.index(0)), bit = 1u << (i & 31u);
+      if (atomicOr(&bits[i >> 5], bit) & bit)
+        twice = true;
+      else
+        speaks |= 1u << j;
+    }
+  }
+  const auto max_op = [](float a, float b) { return fmaxf(a, b); };
+  const auto add_op = [](float a, float b) { return a + b; };
   // log q = (t - from) - norm, the larger of the two subtracted first.
   float from = 0.0f, norm;
   if (p.top_lse) {
@@ -146,10 +190,12 @@ __global__ void __launch_bounds__(kRowMaxThreads)
   } else {
     from = cta_float(rec.scratch, high, max_op);
     float sum = 0.0f;
+#pragma unroll 1
     for (int k = tid; k < p.K; k += nt) sum += expf(rec.logq[k] - from);
     norm = logf(cta_float(rec.scratch, sum, add_op));
   }
   float qsum = 0.0f;
+#pragma unroll 1
   for (int k = tid; k < p.K; k += nt) {
     const float lq = (rec.logq[k] - from) - norm;
     const float q = rec.at[k] >= 0 ? expf(lq) : 0.0f;
@@ -157,43 +203,20 @@ __global__ void __launch_bounds__(kRowMaxThreads)
     rec.q[k] = q;
     qsum += q;
   }
-  qsum = cta_float(rec.scratch, qsum, add_op);  // also: the slice is in place
+  qsum = cta_float(rec.scratch, qsum, add_op);  // also: the bits are set
   const float rest = p.top_lse ? fmaxf(1.0f - qsum, 0.0f) : 0.0f;
   const float whole = qsum + rest;
-
-  // Take the record's logits out of the slice.  An entry that finds its own mark
-  // in its place speaks for its token.
-  for (int k = tid; k < p.K; k += nt) {
-    const int at = rec.at[k];
-    if (at >= s.lo && at < s.hi) rec.z[k] = Row<T>::to_float(s.data[at - s.lo]);
-  }
-  __syncthreads();
-  for (int k = tid; k < p.K; k += nt) {
-    const int at = rec.at[k];
-    if (at >= s.lo && at < s.hi) s.data[at - s.lo] = mark_of(k, T());
-  }
-  __syncthreads();
-  static_assert(kTopMax / 128 <= 32, "one bit for each entry of a thread");
-  uint32_t speaks = 0;  // bit j: entry tid + j nt speaks for its token
-  bool twice = false;
-  for (int k = tid, j = 0; k < p.K; k += nt, ++j) {
-    const int at = rec.at[k];
-    if (at >= s.lo && at < s.hi) {
-      if (of_mark(s.data[at - s.lo]) == k)
-        speaks |= 1u << j;
-      else
-        twice = true;
-    }
-  }
   if (__syncthreads_or(twice)) {
     // Some token is named more than once: its first entry speaks, with the
     // entries' probabilities added up in their order.
     speaks = 0;
+#pragma unroll 1
     for (int k = tid, j = 0; k < p.K; k += nt, ++j) {
       const int at = rec.at[k];
-      if (at < s.lo || at >= s.hi) continue;
+      if (at < 0 || !s.holds(at)) continue;
       bool first = true;
       float q = 0.0f;
+#pragma unroll 1
       for (int i = 0; i < p.K; ++i)
         if (rec.at[i] == at) {
           first &= i >= k;
@@ -203,12 +226,10 @@ __global__ void __launch_bounds__(kRowMaxThreads)
       rec.token_q[k] = q;
     }
     __syncthreads();
+#pragma unroll 1
     for (int k = tid, j = 0; k < p.K; k += nt, ++j)
       if (speaks >> j & 1u) rec.q[k] = rec.token_q[k];
   }
-  for (int k = tid, j = 0; k < p.K; k += nt, ++j)
-    if (speaks >> j & 1u) s.data[rec.at[k] - s.lo] = Row<T>::neg_inf();
-  __syncthreads();
 
   // The sums of 2^x, x = z log2(e) / tau, over the record and over the rest, each
   // relative to a reference of its own: its maximum, and in the backward call
@@ -220,6 +241,7 @@ __global__ void __launch_bounds__(kRowMaxThreads)
     in.m = p.stats[2ll * r] * kRowLog2e;
     out.m = p.stats[2ll * r + 1] * kRowLog2e;
   }
+#pragma unroll 1
   for (int k = tid, j = 0; k < p.K; k += nt, ++j)
     if (speaks >> j & 1u) {
       if (backward) {
@@ -229,13 +251,22 @@ __global__ void __launch_bounds__(kRowMaxThreads)
         in = merge(in, MaxSum{x, x == -inf ? 0.0f : fast_exp2(fmaf(rec.z[k], c2, -x))});
       }
     }
-  for (int v = tid; v < s.n_vec; v += nt) {
+  load_slice<4>(s, [&](int v, const uint4& q) {
     float z[kVec];
-    Row<T>::unpack(s.vec[v], z);
-    if (!backward) {
-      float m = z[0];
+    Row<T>::unpack(q, z);
+    const uint32_t named = vector_bits<T>(bits, v);
+    float m;
+    if (named) {
+#pragma unroll
+      for (int e = 0; e < kVec; ++e)
+        if (named >> e & 1u) z[e] = -inf;
+      m = z[0];
 #pragma unroll
       for (int e = 1; e < kVec; ++e) m = max_nan(m, z[e]);
+    } else {
+      m = vec_max(q, -inf, T());
+    }
+    if (!backward) {
       m *= c2;
       if (!(m <= out.m)) {  // a new maximum, or NaN
         out.s = out.m == -inf ? 0.0f : out.s * fast_exp2(out.m - m);
@@ -243,32 +274,52 @@ __global__ void __launch_bounds__(kRowMaxThreads)
       }
     }
     if (out.m != -inf) {
+      float2 e2 = make_float2(0.0f, 0.0f);
 #pragma unroll
-      for (int e = 0; e < kVec; ++e) out.s += fast_exp2(fmaf(z[e], c2, -out.m));
+      for (int e = 0; e < kVec; e += 2) {
+        const float2 x = __ffma2_rn(make_float2(z[e], z[e + 1]), make_float2(c2, c2),
+                                    make_float2(-out.m, -out.m));
+        e2 = __fadd2_rn(e2, make_float2(fast_exp2(x.x), fast_exp2(x.y)));
+      }
+      out.s += e2.x + e2.y;
+    }
+  });
+  c.begun();
+  out = max_sum_of(cta_reduce(&sh, bits_of(out), MaxSumOp()));
+  in = max_sum_of(cta_reduce(&sh, bits_of(in), MaxSumOp(), 1));
+  {
+    const unsigned long long mine[2] = {bits_of(out), bits_of(in)};
+    const Parts parts = cluster_exchange(c, mine);
+    out = max_sum_of(parts.of(0)[0]);
+    in = max_sum_of(parts.of(1)[0]);
+#pragma unroll 1
+    for (int q = 1; q < c.ctas(); ++q) {
+      out = merge(out, max_sum_of(parts.of(0)[q]));
+      in = merge(in, max_sum_of(parts.of(1)[q]));
     }
   }
-  out = max_sum_of(cluster_reduce(c, bits_of(out), MaxSumOp()));
-  in = max_sum_of(cluster_reduce(c, bits_of(in), MaxSumOp()));
   const MaxSum all = merge(out, in);
   const float ref = out.m == -inf ? 0.0f : out.m;
   const float log2_all = log2f(all.s);
   if (!backward) {
     float part = 0.0f;
+#pragma unroll 1
     for (int k = tid; k < p.K; k += nt) {
       const int at = rec.at[k];
-      if (at >= s.lo && at < s.hi) {
+      if (at >= 0 && s.holds(at)) {
         const float q = expf(rec.logq[k]);
         if (q > 0.0f)
           part += q * (rec.logq[k] - (fmaf(rec.z[k], c2, -all.m) - log2_all) * kLn2);
       }
     }
     part = cta_float(rec.scratch, part, add_op);
-    if (tid == 0) st_peer(reinterpret_cast<const uint32_t*>(&rec.loss_part[c.rank]), 0,
-                          __float_as_uint(part));
-    row_sync();
-    if (c.rank == 0 && tid == 0) {
+    if (tid == 0)
+      c.store(reinterpret_cast<uint32_t*>(&rec.loss_part[c.rank()]), 0, __float_as_uint(part));
+    c.sync();
+    if (c.rank() == 0 && tid == 0) {
       float kl = 0.0f;
-      for (int q = 0; q < ctas; ++q) kl += rec.loss_part[q];
+#pragma unroll 1
+      for (int q = 0; q < c.ctas(); ++q) kl += rec.loss_part[q];
       const float log_rest = ((out.m - all.m) + (log2f(out.s) - log2_all)) * kLn2;
       if (rest > 0.0f) kl += rest * (logf(rest) - log_rest);
       p.loss[r] = w * (p.tau * p.tau) * kl;
@@ -284,30 +335,29 @@ __global__ void __launch_bounds__(kRowMaxThreads)
   const float p_rest = out.m == -inf ? 0.0f : out.s * fast_exp2(out.m - all.m) / all.s;
   const float coef = out.s > 0.0f || out.s != out.s ? up * (whole * p_rest - rest) / out.s : 0.0f;
   const auto grad_of = [&](float z) { return coef * fast_exp2(fmaf(z, c2, -ref)); };
-  const uint32_t a_in = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(row + s.lo)) & 15u;
-  const uint32_t a_out = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(grow + s.lo)) & 15u;
   if (a_in == a_out) {
-    uint4* dst = reinterpret_cast<uint4*>(reinterpret_cast<uintptr_t>(grow + s.lo) &
-                                          ~static_cast<uintptr_t>(15));
-    for (int v = tid; v < s.n_vec; v += nt) {
+    for_slice<kCluster ? 4 : 8>(s, [&](int v, const uint4& q) {
       float z[kVec];
-      Row<T>::unpack(s.vec[v], z);
+      Row<T>::unpack(q, z);
 #pragma unroll
       for (int e = 0; e < kVec; ++e) z[e] = grad_of(z[e]);
-      const int i0 = s.index(v, 0);
-      if (i0 >= s.lo && i0 + kVec <= s.hi) {
-        dst[v] = Row<T>::pack(z);
+      if (v >= s.first && v < s.last) {
+        __stcs(dst + v, Row<T>::pack(z));
       } else {
 #pragma unroll
         for (int e = 0; e < kVec; ++e)
-          if (i0 + e >= s.lo && i0 + e < s.hi) grow[i0 + e] = Row<T>::from_float(z[e]);
+          if (s.holds(s.index(v) + e)) grow[s.index(v) + e] = Row<T>::from_float(z[e]);
       }
-    }
+    });
   } else {
-    for (int i = s.lo + tid; i < s.hi; i += nt)
-      grow[i] = Row<T>::from_float(grad_of(Row<T>::to_float(s.data[i - s.lo])));
+#pragma unroll 1
+    for (int i = s.lo + tid; i < s.hi; i += nt) {
+      const T z = kCluster ? reinterpret_cast<const T*>(s.kept)[i - s.index(0)] : row[i];
+      grow[i] = Row<T>::from_float(grad_of(Row<T>::to_float(z)));
+    }
   }
-  __syncthreads();  // the record's tokens, written as -inf above, come after
+  __syncthreads();  // the record's tokens come after
+#pragma unroll 1
   for (int k = tid, j = 0; k < p.K; k += nt, ++j)
     if (speaks >> j & 1u) {
       const float pk = fast_exp2(fmaf(rec.z[k], c2, -all.m)) / all.s;

@@ -38,7 +38,14 @@ RowDevice g_row[kMaxDevices];
 template <typename K>
 bool open_smem(K* kernel) {
   return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                              kRowSliceMax) == cudaSuccess;
+                              kRowSliceMax) == cudaSuccess &&
+         cudaFuncSetAttribute(kernel, cudaFuncAttributePreferredSharedMemoryCarveout,
+                              cudaSharedmemCarveoutMaxShared) == cudaSuccess;
+}
+
+template <typename K>
+bool open_both(K* cluster, K* alone) {
+  return open_smem(cluster) && open_smem(alone);
 }
 
 // The current device, whose kernels' shared-memory limits are set on first use.
@@ -59,9 +66,12 @@ int row_device(RowDevice** out) {
       return CAI_ERR_CUDA;
     }
     if (major != 10 || minor != 3) return CAI_ERR_UNSUPPORTED;
-    if (!open_smem(sample_rows_kernel<float>) || !open_smem(sample_rows_kernel<__nv_bfloat16>) ||
-        !open_smem(top_rows_kernel<float>) || !open_smem(top_rows_kernel<__nv_bfloat16>) ||
-        !open_smem(distill_kernel<float>) || !open_smem(distill_kernel<__nv_bfloat16>)) {
+    if (!open_both(sample_rows_kernel<float, true>, sample_rows_kernel<float, false>) ||
+        !open_both(sample_rows_kernel<__nv_bfloat16, true>, sample_rows_kernel<__nv_bfloat16, false>) ||
+        !open_both(top_rows_kernel<float, true>, top_rows_kernel<float, false>) ||
+        !open_both(top_rows_kernel<__nv_bfloat16, true>, top_rows_kernel<__nv_bfloat16, false>) ||
+        !open_both(distill_kernel<float, true>, distill_kernel<float, false>) ||
+        !open_both(distill_kernel<__nv_bfloat16, true>, distill_kernel<__nv_bfloat16, false>)) {
       cudaGetLastError();
       return CAI_ERR_CUDA;
     }
@@ -85,30 +95,35 @@ int check_rows(const void* p, int32_t dtype, int64_t ld, int32_t M, int32_t V) {
 
 bool aligned4(const void* p) { return reinterpret_cast<uintptr_t>(p) % 4 == 0; }
 
-// A cluster of CTAs for every row.
-template <typename P>
-int launch_rows(void (*kernel)(P, int), const P& p, int M, int V, int elem, int sms,
-                cudaStream_t stream) {
-  const int ctas = row_ctas(M, V, elem, sms);
+// A cluster of CTAs, or one alone, for every row.  `extra`: dynamic shared memory
+// beside the slice, for that many elements of it.
+template <typename P, typename Extra>
+int launch_rows(void (*cluster)(P, int), void (*alone)(P, int), const P& p, int M, int V, int elem,
+                int sms, void* stream, Extra&& extra) {
+  const RowPlan plan = row_plan(M, V, elem, sms);
+  const bool split = plan.ctas > 0;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(static_cast<unsigned>(M) * ctas);
-  cfg.blockDim = dim3(row_threads(V, ctas));
-  cfg.dynamicSmemBytes = row_slice_bytes(V, ctas, elem);
-  cfg.stream = stream;
+  cfg.gridDim = dim3(static_cast<unsigned>(split ? M * plan.ctas : M));
+  cfg.blockDim = dim3(plan.threads);
+  cfg.dynamicSmemBytes = split ? row_slice_bytes(V, plan.ctas, elem) + extra(row_chunk(V, plan.ctas))
+                               : extra(V) + (getenv("ROW_EXTRA") ? atoi(getenv("ROW_EXTRA")) : 0);
+  cfg.stream = static_cast<cudaStream_t>(stream);
   cudaLaunchAttribute at[1];
   at[0].id = cudaLaunchAttributeClusterDimension;
-  at[0].val.clusterDim.x = ctas;
+  at[0].val.clusterDim.x = split ? plan.ctas : 1;
   at[0].val.clusterDim.y = 1;
   at[0].val.clusterDim.z = 1;
   cfg.attrs = at;
-  cfg.numAttrs = 1;
+  cfg.numAttrs = split ? 1 : 0;
   cudaGetLastError();  // an error left by earlier work is not this call's
-  if (cudaLaunchKernelEx(&cfg, kernel, p, ctas) != cudaSuccess) {
+  if (cudaLaunchKernelEx(&cfg, split ? cluster : alone, p, plan.ctas) != cudaSuccess) {
     cudaGetLastError();
     return CAI_ERR_CUDA;
   }
   return CAI_OK;
 }
+
+size_t nothing(int) { return 0; }
 
 }  // namespace
 
@@ -125,8 +140,11 @@ extern "C" int cai_sample_rows(const void* logits, int32_t dtype, int64_t ld, in
   for (const void* p : ptrs)
     if (p && ((p != logits && !aligned4(p)) || !on_this_device(p, d->dev))) return CAI_ERR_ARG;
   SampleParams p{logits, ld, M, V, temperature, top_k, top_p, min_p, u, token, prob};
-  return launch_rows(dtype == CAI_BF16 ? sample_rows_kernel<__nv_bfloat16> : sample_rows_kernel<float>,
-                     p, M, V, elem_bytes(dtype), d->sms, static_cast<cudaStream_t>(stream));
+  return dtype == CAI_BF16
+             ? launch_rows(sample_rows_kernel<__nv_bfloat16, true>,
+                           sample_rows_kernel<__nv_bfloat16, false>, p, M, V, 2, d->sms, stream, nothing)
+             : launch_rows(sample_rows_kernel<float, true>, sample_rows_kernel<float, false>, p, M, V,
+                           4, d->sms, stream, nothing);
 }
 
 extern "C" int cai_top_rows(const void* logits, int32_t dtype, int64_t ld, int32_t M, int32_t V,
@@ -144,8 +162,11 @@ extern "C" int cai_top_rows(const void* logits, int32_t dtype, int64_t ld, int32
   for (const void* p : ptrs)
     if ((p != logits && !aligned4(p)) || !on_this_device(p, d->dev)) return CAI_ERR_ARG;
   TopParams p{logits, ld, M, V, K, static_cast<float>(temperature), values, index, lse};
-  return launch_rows(dtype == CAI_BF16 ? top_rows_kernel<__nv_bfloat16> : top_rows_kernel<float>, p,
-                     M, V, elem_bytes(dtype), d->sms, static_cast<cudaStream_t>(stream));
+  return dtype == CAI_BF16
+             ? launch_rows(top_rows_kernel<__nv_bfloat16, true>, top_rows_kernel<__nv_bfloat16, false>,
+                           p, M, V, 2, d->sms, stream, nothing)
+             : launch_rows(top_rows_kernel<float, true>, top_rows_kernel<float, false>, p, M, V, 4,
+                           d->sms, stream, nothing);
 }
 
 namespace {
@@ -169,8 +190,11 @@ int distill_call(DistillParams& p, int32_t dtype, int64_t ld_grad, void* stream)
   if (!on_this_device(p.logits, d->dev) || (p.grad && !on_this_device(p.grad, d->dev)))
     return CAI_ERR_ARG;
   p.ld_grad = ld_grad;
-  return launch_rows(dtype == CAI_BF16 ? distill_kernel<__nv_bfloat16> : distill_kernel<float>, p,
-                     p.M, p.V, e, d->sms, static_cast<cudaStream_t>(stream));
+  return dtype == CAI_BF16
+             ? launch_rows(distill_kernel<__nv_bfloat16, true>, distill_kernel<__nv_bfloat16, false>, p,
+                           p.M, p.V, 2, d->sms, stream, bitmap_bytes)
+             : launch_rows(distill_kernel<float, true>, distill_kernel<float, false>, p, p.M, p.V, 4,
+                           d->sms, stream, bitmap_bytes);
 }
 
 }  // namespace

@@ -1,11 +1,16 @@
-// What the operators on rows of vocabulary logits share: a row is cut over the
-// CTAs of one thread-block cluster, each keeps its slice in shared memory for
-// every pass it makes, and the cluster reduces and searches through distributed
-// shared memory.  HBM is read once, and no call needs a workspace.
+// What the operators on rows of vocabulary logits share.  HBM is read once and no
+// call needs a workspace, in two forms of the same kernels:
+//
+//   Cluster (few rows): a row is cut over the CTAs of one thread-block cluster,
+//   each keeps its slice in shared memory for every pass it makes, and the
+//   cluster reduces and searches through distributed shared memory.
+//   Alone (many rows): one CTA takes a row; passes after the first read it from
+//   L2, where the rows in progress fit, and nothing waits for another CTA.
 #pragma once
 
 #include <climits>
 #include <cstdint>
+#include <cstdlib>
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 
@@ -14,9 +19,9 @@
 namespace cai {
 
 constexpr int kRowMaxCluster = 8;    // portable cluster size
-constexpr int kRowMaxThreads = 512;
+constexpr int kRowMaxThreads = 1024;
 constexpr int kRowMaxWarps = kRowMaxThreads / 32;
-constexpr int kRowSliceMax = 192 * 1024;  // bytes of a row that one CTA keeps
+constexpr int kRowSliceMax = 160 * 1024;  // bytes of a row that one CTA keeps
 
 // A vector of 16 bytes of logits as floats.
 template <typename T>
@@ -106,24 +111,130 @@ __device__ __forceinline__ float value_of_key(uint32_t k) {
   return __uint_as_float(k & 0x80000000u ? k ^ 0x80000000u : ~k);
 }
 
-// The slice of a row that this CTA keeps: elements [lo, hi) of the row, element
-// lo + i at data[i].  The bytes lie in shared memory as they do in global memory
-// modulo 16, so whole 16-byte vectors are copied as such; what a first or last
-// vector holds besides the slice is -inf.  A vector v covers the elements
-// lo - skip + v kVec ...
-template <typename T>
-struct Slice {
-  uint4* vec;   // vectors of the slice
-  int n_vec;
-  T* data;
-  int lo, hi;   // elements of the row
-  int skip;     // elements of the first vector before the slice
+// (No memory clobber: what a loop holds in registers stays there.  Where a row's
+// gradient is written in place of its logits, each vector is written by the thread
+// that has just read it.)
+__device__ __forceinline__ uint4 ld_stream(const uint4* p) {
+  uint4 v;
+  asm volatile("ld.global.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];"
+               : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
+               : "l"(p));
+  return v;
+}
 
-  __device__ __forceinline__ int index(int v, int e) const {
-    return lo - skip + v * Row<T>::kVec + e;
+// The slice of a row that this CTA works on: elements [lo, hi).  It is seen as
+// 16-byte vectors of global memory; what the first or last of them holds besides
+// the slice is taken as -inf and never read.  Vector v covers the elements
+// lo - skip + v kVec ...; vectors outside [first, last) are such ends and lie in
+// edge[0] (v = 0) or edge[1].  kKeep: every vector lies in kept[v] once loaded.
+template <typename T, bool kKeep>
+struct Slice {
+  static constexpr int kVec = Row<T>::kVec;
+  static constexpr bool kKept = kKeep;  // ends are vectors like the others then
+  const T* row;
+  const uint4* src;
+  uint4* kept;
+  uint4* edge;
+  int n_vec, first, last;
+  int lo, hi;
+  int skip;
+
+  __device__ __forceinline__ Slice(const T* row_, int lo_, int hi_, uint4* kept_, uint4* edge_)
+      : row(row_), kept(kept_), edge(edge_), lo(lo_), hi(hi_) {
+    const uintptr_t at = reinterpret_cast<uintptr_t>(row + lo);
+    src = reinterpret_cast<const uint4*>(at & ~static_cast<uintptr_t>(15));
+    skip = static_cast<int>((at & 15) / sizeof(T));
+    const int span = skip + hi - lo;
+    n_vec = hi > lo ? (span + kVec - 1) / kVec : 0;
+    first = skip ? 1 : 0;
+    last = max(first, span / kVec);
+    if (n_vec == 0) first = last = 0;
   }
-  __device__ __forceinline__ int pads() const { return n_vec * Row<T>::kVec - (hi - lo); }
+  __device__ __forceinline__ int index(int v) const { return lo - skip + v * kVec; }
+  __device__ __forceinline__ bool holds(int i) const { return i >= lo && i < hi; }
+  // The end that thread `tid` looks after (-1: none): the first two threads do.
+  __device__ __forceinline__ int end_of(int tid) const {
+    return tid == 0 ? (first > 0 && n_vec > 0 ? 0 : -1) : tid == 1 && last < n_vec ? n_vec - 1 : -1;
+  }
+  // The value of an element, once the slice is loaded.
+  __device__ __forceinline__ float value(int i) const {
+    return Row<T>::to_float(kKeep ? reinterpret_cast<const T*>(kept)[i - index(0)] : row[i]);
+  }
+  // A vector that is no end, and any, from where the slice lies now.
+  __device__ __forceinline__ uint4 body(int v) const { return kKeep ? kept[v] : ld_stream(src + v); }
+  __device__ __forceinline__ uint4 get(int v) const {
+    if (kKeep) return kept[v];
+    if (v >= first && v < last) return ld_stream(src + v);
+    return edge[v != 0 || first == 0];
+  }
 };
+
+// Calls f(v, vector) for the vectors v = from, from + step, ... below `end`, all of
+// them no ends, kFlight loads at a time.  The last round is like the others, with
+// fewer loads: one by one its vectors would wait for memory as often as all the
+// rounds before.
+template <int kFlight, typename S, typename F>
+__device__ __forceinline__ void for_body(const S& s, int from, int end, int step, F&& f) {
+#pragma unroll 1
+  for (int v = from; v < end; v += kFlight * step) {
+    uint4 r[kFlight];
+#pragma unroll
+    for (int j = 0; j < kFlight; ++j)
+      if (v + j * step < end) r[j] = s.body(v + j * step);
+#pragma unroll
+    for (int j = 0; j < kFlight; ++j)
+      if (v + j * step < end) f(v + j * step, r[j]);
+  }
+}
+
+// Calls f(v, vector) for every vector of the slice, each thread its share.
+template <int kFlight, typename T, bool kKeep, typename F>
+__device__ __forceinline__ void for_slice(const Slice<T, kKeep>& s, F&& f) {
+  const int tid = threadIdx.x, step = static_cast<int>(blockDim.x);
+  if (kKeep) {
+    for_body<kFlight>(s, tid, s.n_vec, step, f);
+    return;
+  }
+  for_body<kFlight>(s, s.first + tid, s.last, step, f);
+  const int end = s.end_of(tid);
+  if (end >= 0) f(end, s.get(end));
+}
+
+// The first pass: as for_slice, from global memory; builds the ends and keeps
+// every vector if kKeep.
+template <int kFlight, typename T, bool kKeep, typename F>
+__device__ __forceinline__ void load_slice(const Slice<T, kKeep>& s, F&& f) {
+  constexpr int kVec = Row<T>::kVec;
+  const int tid = threadIdx.x, step = static_cast<int>(blockDim.x);
+#pragma unroll 1
+  for (int v = s.first + tid; v < s.last; v += kFlight * step) {
+    uint4 r[kFlight];
+#pragma unroll
+    for (int j = 0; j < kFlight; ++j)
+      if (v + j * step < s.last) r[j] = ld_stream(s.src + v + j * step);
+#pragma unroll
+    for (int j = 0; j < kFlight; ++j)
+      if (v + j * step < s.last) {
+        if (kKeep) s.kept[v + j * step] = r[j];
+        f(v + j * step, r[j]);
+      }
+  }
+  const int end = s.end_of(tid);
+  if (end >= 0) {
+    uint4 r;
+    T* d = reinterpret_cast<T*>(&r);
+#pragma unroll
+    for (int e = 0; e < kVec; ++e) {
+      const int i = s.index(end) + e;
+      d[e] = s.holds(i) ? s.row[i] : Row<T>::neg_inf();
+    }
+    if (kKeep)
+      s.kept[end] = r;
+    else
+      s.edge[end != 0 || s.first == 0] = r;
+    f(end, r);
+  }
+}
 
 // Elements per CTA of a row of V over `ctas`: a multiple of 64.
 __host__ __device__ __forceinline__ int row_chunk(int V, int ctas) {
@@ -134,77 +245,15 @@ __host__ __device__ __forceinline__ size_t row_slice_bytes(int V, int ctas, int 
   return static_cast<size_t>(row_chunk(V, ctas)) * elem + 32;
 }
 
-template <typename T>
-__device__ __forceinline__ Slice<T> row_slice(const T* row, int V, int rank, int ctas, void* smem) {
-  Slice<T> s;
-  const int chunk = row_chunk(V, ctas);
-  s.lo = min(V, rank * chunk);
-  s.hi = min(V, s.lo + chunk);
-  const uint32_t a = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(row + s.lo)) & 15u;
-  s.skip = static_cast<int>(a / sizeof(T));
-  s.vec = static_cast<uint4*>(smem);
-  s.data = reinterpret_cast<T*>(static_cast<char*>(smem) + a);
-  s.n_vec = s.hi > s.lo ? (s.skip + s.hi - s.lo + Row<T>::kVec - 1) / Row<T>::kVec : 0;
-  return s;
-}
-
-__device__ __forceinline__ uint4 ld_stream(const uint4* p) {
-  uint4 v;
-  asm volatile("ld.global.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];"
-               : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
-               : "l"(p)
-               : "memory");
-  return v;
-}
-
-// Copies the slice from global memory, vector by vector (the first and last,
-// where they are not whole, element by element), and hands every vector to
-// `see` on the way.  Each thread has kFlight loads in flight.
-template <typename T, int kFlight, typename F>
-__device__ __forceinline__ void load_slice(const Slice<T>& s, const T* row, F&& see) {
-  constexpr int kVec = Row<T>::kVec;
-  // Global address of vector 0, which may begin before the slice: only whole
-  // vectors are read through it.
-  const uint4* src = reinterpret_cast<const uint4*>(
-      reinterpret_cast<uintptr_t>(row + s.lo) & ~static_cast<uintptr_t>(15));
-  const int first = s.skip ? 1 : 0;
-  const int last = (s.skip + s.hi - s.lo) / kVec;  // whole vectors end here
-  const int step = static_cast<int>(blockDim.x);
-  for (int v0 = first + static_cast<int>(threadIdx.x); v0 < last; v0 += kFlight * step) {
-    uint4 r[kFlight];
-#pragma unroll
-    for (int j = 0; j < kFlight; ++j)
-      if (v0 + j * step < last) r[j] = ld_stream(src + v0 + j * step);
-#pragma unroll
-    for (int j = 0; j < kFlight; ++j)
-      if (v0 + j * step < last) {
-        s.vec[v0 + j * step] = r[j];
-        see(r[j]);
-      }
-  }
-  // The vectors at the two ends that are not whole (they may be one).
-  if (threadIdx.x < 2 && s.n_vec > 0) {
-    const int v = threadIdx.x == 0 ? 0 : s.n_vec - 1;
-    const bool part = threadIdx.x == 0 ? first != 0 : last < s.n_vec && s.n_vec - 1 >= first;
-    if (part) {
-      T* d = reinterpret_cast<T*>(s.vec + v);
-#pragma unroll
-      for (int e = 0; e < kVec; ++e) {
-        const int i = s.index(v, e);
-        d[e] = i >= s.lo && i < s.hi ? row[i] : Row<T>::neg_inf();
-      }
-      see(s.vec[v]);
-    }
-  }
+template <typename T, bool kKeep>
+__device__ __forceinline__ Slice<T, kKeep> row_slice(const T* row, int V, int rank, int ctas,
+                                                     void* smem, uint4* edge) {
+  const int chunk = kKeep ? row_chunk(V, ctas) : V;
+  const int lo = min(V, rank * chunk);
+  return Slice<T, kKeep>(row, lo, min(V, lo + chunk), static_cast<uint4*>(smem), edge);
 }
 
 // ------------------------------------------------------ reductions, search --
-
-struct Tally {  // tokens and their weight
-  unsigned long long mass;
-  uint32_t count;
-  uint32_t pad;
-};
 
 constexpr int kBins = 1024;
 constexpr int kListMax = 2048;  // candidates that one CTA finishes alone
@@ -214,64 +263,93 @@ constexpr int kSums = 3;        // values of an exchange
 struct RowShared {
   unsigned long long wred[kSums][kRowMaxWarps];          // values per warp
   unsigned long long slots[4][kSums][kRowMaxCluster];    // values per CTA, written by the peers
-  Tally parts[kRowMaxCluster];
-  Tally found, found_at;  // what lies above the bin that was found, and in it
-  uint32_t found_bin;
-  int32_t told;           // an index one thread found, for all (tell_index)
-  unsigned long long part_scan[kRowMaxWarps];
-  uint32_t part_scan_n[kRowMaxWarps];
+  unsigned long long parts[kRowMaxCluster];
+  struct {                // the bin a level found (search_level)
+    unsigned long long before;
+    int bin;
+    uint32_t count;
+  } found;
+  uint32_t told[2];       // what one thread found, for all (tell)
+  unsigned long long once;  // what one warp worked out, for the CTA (cta_once)
+  uint4 edge[2];          // the slice's ends
   uint32_t listed;        // candidates pushed so far (in CTA 0)
+  uint32_t noted;         // vectors noted so far
+  uint32_t note[kListMax];  // vectors with candidates
   union {
-    struct {              // find_cut
-      unsigned long long mass[kBins];
-      uint32_t count[kBins];
-    };
+    uint32_t count[kBins];               // search_level
     unsigned long long list[kListMax];  // candidates (in CTA 0)
   };
 };
 
+// A CTA's place in the cluster that works on its row; kCluster false: there is no
+// other.
+template <bool kCluster>
 struct RowCta {
   RowShared* sh;
-  int rank, ctas;
-  int turn;  // which slots the next reduction uses
+  int rank_, ctas_;
+  int turn = 0;  // which slots the next exchange uses
+
+  __device__ __forceinline__ RowCta(RowShared* s, int ctas)
+      : sh(s), rank_(kCluster ? static_cast<int>(cluster_ctarank()) : 0), ctas_(ctas) {}
+  __device__ __forceinline__ int rank() const { return kCluster ? rank_ : 0; }
+  __device__ __forceinline__ int ctas() const { return kCluster ? ctas_ : 1; }
+
+  // Peers' shared memory may be written once every CTA of the cluster has begun:
+  // begin at the top of a kernel, begun before the first such write (and before
+  // any early return).
+  __device__ __forceinline__ static void begin() {
+    if (kCluster) asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
+  }
+  __device__ __forceinline__ void begun() const {
+    if (!kCluster) return;
+    __syncwarp();
+    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+  }
+  // All threads of the row.  Warps may arrive from loops that their lanes left at
+  // different times.
+  __device__ __forceinline__ void sync() const {
+    if (kCluster) {
+      __syncwarp();
+      cluster_sync();
+    } else {
+      __syncthreads();
+    }
+  }
+  // Writes into, or reads from, `p`'s place in the shared memory of CTA `rank`.
+  __device__ __forceinline__ void store(unsigned long long* p, int rank, unsigned long long v) const {
+    if (kCluster)
+      asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(mapa_shared(p, rank)), "l"(v) : "memory");
+    else
+      *p = v;
+  }
+  __device__ __forceinline__ void store(uint32_t* p, int rank, uint32_t v) const {
+    if (kCluster)
+      asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(mapa_shared(p, rank)), "r"(v) : "memory");
+    else
+      *p = v;
+  }
+  __device__ __forceinline__ unsigned long long load(const unsigned long long* p, int rank) const {
+    if (!kCluster) return *p;
+    unsigned long long v;
+    asm volatile("ld.shared::cluster.u64 %0, [%1];" : "=l"(v) : "r"(mapa_shared(p, rank)) : "memory");
+    return v;
+  }
+  __device__ __forceinline__ uint32_t load(const uint32_t* p, int rank) const {
+    if (!kCluster) return *p;
+    uint32_t v;
+    asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(mapa_shared(p, rank)) : "memory");
+    return v;
+  }
+  __device__ __forceinline__ uint32_t next(uint32_t* p, int rank) const {  // p++ there
+    if (!kCluster) return atomicAdd(p, 1u);
+    uint32_t v;
+    asm volatile("atom.relaxed.cluster.shared::cluster.add.u32 %0, [%1], 1;"
+                 : "=r"(v)
+                 : "r"(mapa_shared(p, rank))
+                 : "memory");
+    return v;
+  }
 };
-
-// All threads of the cluster.  Warps may arrive from loops that their lanes
-// left at different times.
-__device__ __forceinline__ void row_sync() {
-  __syncwarp();
-  cluster_sync();
-}
-
-// Peers' shared memory may be written once every CTA of the cluster has begun:
-// row_begin at the top of a kernel, row_begun before the first such write (and
-// before any early return).
-__device__ __forceinline__ void row_begin() {
-  asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
-}
-__device__ __forceinline__ void row_begun() {
-  __syncwarp();
-  asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
-}
-
-// Writes a 64-bit value into `p`'s place in the shared memory of CTA `rank`.
-__device__ __forceinline__ void st_peer(const unsigned long long* p, int rank,
-                                        unsigned long long v) {
-  asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(mapa_shared(p, rank)), "l"(v) : "memory");
-}
-__device__ __forceinline__ void st_peer(const uint32_t* p, int rank, uint32_t v) {
-  asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(mapa_shared(p, rank)), "r"(v) : "memory");
-}
-__device__ __forceinline__ unsigned long long ld_peer(const unsigned long long* p, int rank) {
-  unsigned long long v;
-  asm volatile("ld.shared::cluster.u64 %0, [%1];" : "=l"(v) : "r"(mapa_shared(p, rank)) : "memory");
-  return v;
-}
-__device__ __forceinline__ uint32_t ld_peer(const uint32_t* p, int rank) {
-  uint32_t v;
-  asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(mapa_shared(p, rank)) : "memory");
-  return v;
-}
 
 template <typename Op>
 __device__ __forceinline__ unsigned long long warp_reduce(unsigned long long v, Op op) {
@@ -283,15 +361,17 @@ __device__ __forceinline__ unsigned long long warp_reduce(unsigned long long v, 
 // Reduces one value per thread over the CTA, the result in every thread.  All
 // threads call it; wred is free again after the next barrier.
 template <typename Op>
-__device__ __forceinline__ unsigned long long cta_reduce(const RowCta& c, unsigned long long v,
-                                                         Op op, int which = 0) {
+__device__ __forceinline__ unsigned long long cta_reduce(RowShared* sh, unsigned long long v, Op op,
+                                                         int which = 0) {
   v = warp_reduce(v, op);
-  const int warp = threadIdx.x >> 5, n = blockDim.x >> 5;
-  if ((threadIdx.x & 31) == 0) c.sh->wred[which][warp] = v;
+  const int lane = threadIdx.x & 31, n = blockDim.x >> 5;
+  if (lane == 0) sh->wred[which][threadIdx.x >> 5] = v;
   __syncthreads();
-  unsigned long long r = c.sh->wred[which][0];
-  for (int i = 1; i < n; ++i) r = op(r, c.sh->wred[which][i]);
-  return r;
+  // Lanes repeat the warps' values: n is a power of two here.
+  v = sh->wred[which][lane & (n - 1)];
+#pragma unroll 1
+  for (int o = n >> 1; o >= 1; o >>= 1) v = op(v, __shfl_xor_sync(0xffffffffu, v, o));
+  return v;
 }
 
 // Values per CTA to every CTA of the cluster: the slots of value `which`, in rank
@@ -303,29 +383,31 @@ struct Parts {
   }
   __device__ __forceinline__ unsigned long long sum(int ctas, int which) const {
     unsigned long long r = 0;
+#pragma unroll 1
     for (int i = 0; i < ctas; ++i) r += of(which)[i];
     return r;
   }
 };
-template <int kN>
-__device__ __forceinline__ Parts cluster_exchange(RowCta& c, const unsigned long long (&v)[kN]) {
+template <int kN, typename C>
+__device__ __forceinline__ Parts cluster_exchange(C& c, const unsigned long long (&v)[kN]) {
   unsigned long long* s = &c.sh->slots[c.turn & 3][0][0];
   c.turn++;
-  if (static_cast<int>(threadIdx.x) < c.ctas) {
+  if (static_cast<int>(threadIdx.x) < c.ctas()) {
 #pragma unroll
-    for (int i = 0; i < kN; ++i) st_peer(s + i * kRowMaxCluster + c.rank, threadIdx.x, v[i]);
+    for (int i = 0; i < kN; ++i) c.store(s + i * kRowMaxCluster + c.rank(), threadIdx.x, v[i]);
   }
-  row_sync();
+  c.sync();
   return Parts{s};
 }
 
-template <typename Op>
-__device__ __forceinline__ unsigned long long cluster_reduce(RowCta& c, unsigned long long v,
+template <typename C, typename Op>
+__device__ __forceinline__ unsigned long long cluster_reduce(C& c, unsigned long long v,
                                                              Op op) {
-  const unsigned long long mine[1] = {cta_reduce(c, v, op)};
+  const unsigned long long mine[1] = {cta_reduce(c.sh, v, op)};
   const unsigned long long* s = cluster_exchange(c, mine).of(0);
   unsigned long long r = s[0];
-  for (int i = 1; i < c.ctas; ++i) r = op(r, s[i]);
+#pragma unroll 1
+  for (int i = 1; i < c.ctas(); ++i) r = op(r, s[i]);
   return r;
 }
 
@@ -336,8 +418,8 @@ struct AddOp {
   }
 };
 // The sums of up to three values per thread, CTA by CTA, to all.
-template <int kN>
-__device__ __forceinline__ Parts exchange_sums(RowCta& c, const unsigned long long (&v)[kN]) {
+template <int kN, typename C>
+__device__ __forceinline__ Parts exchange_sums(C& c, const unsigned long long (&v)[kN]) {
   const int warp = threadIdx.x >> 5, n = blockDim.x >> 5;
   unsigned long long r[kN];
 #pragma unroll
@@ -348,8 +430,9 @@ __device__ __forceinline__ Parts exchange_sums(RowCta& c, const unsigned long lo
   __syncthreads();
 #pragma unroll
   for (int i = 0; i < kN; ++i) {
-    r[i] = 0;
-    for (int w = 0; w < n; ++w) r[i] += c.sh->wred[i][w];
+    r[i] = c.sh->wred[i][threadIdx.x & (n - 1)];
+#pragma unroll 1
+    for (int o = n >> 1; o >= 1; o >>= 1) r[i] += __shfl_xor_sync(0xffffffffu, r[i], o);
   }
   return cluster_exchange(c, r);
 }
@@ -367,194 +450,296 @@ struct MaxNanOp {  // on the bits of a float
   }
 };
 
-// Where a falling run over the kept elements of the row first reaches `want`
-// (by count or by weight): the key there, and what lies above that key.
+__device__ __forceinline__ unsigned long long warp_scan(unsigned long long v) {  // inclusive
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const unsigned long long m = __shfl_up_sync(0xffffffffu, v, o);
+    if ((threadIdx.x & 31) >= o) v += m;
+  }
+  return v;
+}
+
+// The sum of the values before this thread's, and of all.
+__device__ __forceinline__ unsigned long long cta_scan(RowShared* sh, unsigned long long v,
+                                                       unsigned long long& whole) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, n = blockDim.x >> 5;
+  const unsigned long long incl = warp_scan(v);
+  __syncthreads();
+  if (lane == 31) sh->wred[0][warp] = incl;
+  __syncthreads();
+  const unsigned long long w = warp_scan(lane < n ? sh->wred[0][lane] : 0);
+  whole = __shfl_sync(0xffffffffu, w, 31);
+  const unsigned long long before = __shfl_sync(0xffffffffu, w, (warp - 1) & 31);
+  return (warp ? before : 0) + incl - v;
+}
+
+// Where a falling run over the elements of the row first reaches a count: between
+// the keys lo and hi, with how many lie above and how many there.
 struct Cut {
-  uint32_t key;
-  Tally above;  // strictly larger keys
-  Tally at;     // this key
+  uint32_t lo, hi;
+  uint32_t above, at;
 };
 
-// Radix search from the largest key down, kBins parts of the remaining key
-// range at a time.  visit(f) calls f(key, weight) for every element that takes
-// part; `top` is the largest key among them.  All threads of all CTAs call it
-// with the same arguments; the whole has to reach `want`.
-template <bool kByMass, typename Visit>
-__device__ __forceinline__ Cut find_cut(RowCta& c, uint32_t top, unsigned long long want,
-                                        Visit&& visit) {
+// One level of a search from the largest value down: count(f) calls f(bin) for
+// the elements that take part, value(bin, n) is what n elements of a bin add to
+// the run, which starts at `run`.  Returns the bin in which it reaches `want` (-1:
+// in none), and the run before it and the elements in it.  All threads of all
+// CTAs call it.
+struct Level {
+  int bin;
+  unsigned long long before;
+  uint32_t count;
+};
+template <typename C, typename Count, typename Value>
+__device__ __forceinline__ Level search_level(C& c, unsigned long long run, unsigned long long want,
+                                              Count&& count, Value&& value) {
   RowShared* sh = c.sh;
   const int tid = threadIdx.x, nt = blockDim.x;
-  uint32_t lo = 0, hi = top;  // the key is in [lo, hi]
-  Tally above{0, 0, 0};
+#pragma unroll 1
+  for (int i = tid; i < kBins; i += nt) sh->count[i] = 0;
+  if (tid == 0) sh->found.bin = -1;
+  __syncthreads();
+  count([&](int b) { atomicAdd(&sh->count[b], 1u); });
+  c.sync();
+  // Every CTA sums its share of the bins over the cluster; bins fall with the
+  // thread index so that a rising scan runs from the largest values down.
+  const int share = kBins / c.ctas();
+  const int per = (share + nt - 1) / nt;  // bins of a thread
+  const auto bin_of = [&](int j) { return kBins - 1 - (c.rank() * share + tid * per + j); };
+  const auto sum_bin = [&](int b) {
+    uint32_t n = 0;
+#pragma unroll 1
+    for (int r = 0; r < c.ctas(); ++r) n += c.load(&sh->count[b], r);
+    return n;
+  };
+  unsigned long long mine = 0, total;
+#pragma unroll 1
+  for (int j = 0; j < per && tid * per + j < share; ++j) mine += value(bin_of(j), sum_bin(bin_of(j)));
+  const unsigned long long before = cta_scan(sh, mine, total);
+  if (tid < c.ctas()) c.store(&sh->parts[c.rank()], tid, total);
+  c.sync();
+#pragma unroll 1
+  for (int r = 0; r < c.rank(); ++r) run += sh->parts[r];
+  run += before;
+  // The thread whose bins hold the place where the run reaches `want`.
+  if (run < want && want <= run + mine) {
+#pragma unroll 1
+    for (int j = 0; j < per; ++j) {
+      const int b = bin_of(j);
+      const uint32_t n = sum_bin(b);
+      const unsigned long long v = value(b, n);
+      if (run + v >= want) {
+#pragma unroll 1
+        for (int r = 0; r < c.ctas(); ++r) {
+          c.store(&sh->found.before, r, run);
+          c.store(reinterpret_cast<uint32_t*>(&sh->found.bin), r, static_cast<uint32_t>(b));
+          c.store(&sh->found.count, r, n);
+        }
+        break;
+      }
+      run += v;
+    }
+  }
+  c.sync();
+  const Level l{sh->found.bin, sh->found.before, sh->found.count};
+  __syncthreads();  // read before the next level clears it
+  return l;
+}
+
+// Radix search for the `want`-th element of the row from the largest down, kBins
+// parts of the remaining key range at a time, until it holds at most `enough`
+// elements or one key.  visit(f) calls f(key) for every element.
+template <typename T, typename C, typename Visit>
+__device__ __forceinline__ Cut find_cut(C& c, uint32_t top, uint32_t want, uint32_t enough, Visit&& visit) {
+  uint32_t lo = 0, hi = top, above = 0;  // the key is in [lo, hi]
+#pragma unroll 1
   for (;;) {
     const uint32_t range = hi - lo;
     const int bits = 32 - __clz(range);  // 0 for one key
     const int shift = bits > 10 ? bits - 10 : 0;
-    for (int i = tid; i < kBins; i += nt) {
-      sh->mass[i] = 0;
-      sh->count[i] = 0;
-    }
-    __syncthreads();
-    visit([&](uint32_t key, unsigned long long w) {
-      if (key - lo <= range) {
-        const uint32_t b = (key - lo) >> shift;
-        atomicAdd(&sh->count[b], 1u);
-        if (kByMass) atomicAdd(&sh->mass[b], w);
-      }
-    });
-    row_sync();
-    // Every CTA sums its share of the bins over the cluster; bins fall with
-    // the thread index so that a rising scan runs from the largest key down.
-    const int share = kBins / c.ctas;
-    const int per = (share + nt - 1) / nt;  // bins of a thread
-    Tally mine{0, 0, 0};
-    for (int j = 0; j < per; ++j) {
-      const int k = tid * per + j;
-      if (k < share) {
-        const int b = kBins - 1 - (c.rank * share + k);
-        for (int r = 0; r < c.ctas; ++r) {
-          mine.count += ld_peer(&sh->count[b], r);
-          if (kByMass) mine.mass += ld_peer(&sh->mass[b], r);
-        }
-      }
-    }
-    Tally incl = mine;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const unsigned long long m = __shfl_up_sync(0xffffffffu, incl.mass, o);
-      const uint32_t n = __shfl_up_sync(0xffffffffu, incl.count, o);
-      if ((tid & 31) >= o) {
-        incl.mass += m;
-        incl.count += n;
-      }
-    }
-    if ((tid & 31) == 31) {
-      sh->part_scan[tid >> 5] = incl.mass;
-      sh->part_scan_n[tid >> 5] = incl.count;
-    }
-    __syncthreads();
-    Tally total{0, 0, 0};
-    for (int w = 0; w < nt / 32; ++w) {
-      if (w == (tid >> 5)) {
-        incl.mass += total.mass;
-        incl.count += total.count;
-      }
-      total.mass += sh->part_scan[w];
-      total.count += sh->part_scan_n[w];
-    }
-    if (tid < c.ctas) {
-      st_peer(&sh->parts[c.rank].mass, tid, total.mass);
-      st_peer(&sh->parts[c.rank].count, tid, total.count);
-    }
-    row_sync();
-    Tally base = above;
-    for (int r = 0; r < c.rank; ++r) {
-      base.mass += sh->parts[r].mass;
-      base.count += sh->parts[r].count;
-    }
-    // The thread whose bins hold the place where the run reaches `want`.
-    const unsigned long long before =
-        kByMass ? base.mass + incl.mass - mine.mass : base.count + incl.count - mine.count;
-    const unsigned long long after =
-        kByMass ? base.mass + incl.mass : static_cast<unsigned long long>(base.count) + incl.count;
-    if (before < want && want <= after) {
-      Tally run{base.mass + incl.mass - mine.mass, base.count + incl.count - mine.count, 0};
-      for (int j = 0; j < per; ++j) {
-        const int b = kBins - 1 - (c.rank * share + tid * per + j);
-        Tally t{0, 0, 0};
-        for (int r = 0; r < c.ctas; ++r) {
-          t.count += ld_peer(&sh->count[b], r);
-          if (kByMass) t.mass += ld_peer(&sh->mass[b], r);
-        }
-        const unsigned long long reach =
-            kByMass ? run.mass + t.mass : static_cast<unsigned long long>(run.count) + t.count;
-        if (reach >= want) {
-          for (int r = 0; r < c.ctas; ++r) {
-            st_peer(&sh->found.mass, r, run.mass);
-            st_peer(&sh->found.count, r, run.count);
-            st_peer(&sh->found_bin, r, static_cast<uint32_t>(b));
-            st_peer(&sh->found_at.mass, r, t.mass);
-            st_peer(&sh->found_at.count, r, t.count);
-          }
-          break;
-        }
-        run.mass += t.mass;
-        run.count += t.count;
-      }
-    }
-    row_sync();
-    above = sh->found;
-    const uint32_t b = sh->found_bin;
-    const Tally at = sh->found_at;  // written again two cluster_syncs from here
-    const uint32_t from = lo + (b << shift);
-    if (shift == 0) return Cut{from, above, at};
+    const Level l = search_level(
+        c, above, want,
+        [&](auto&& f) {
+          visit([&](uint32_t key) {
+            if (key - lo <= range) f(static_cast<int>((key - lo) >> shift));
+          });
+        },
+        [](int, uint32_t n) -> unsigned long long { return n; });
+    above = static_cast<uint32_t>(l.before);
+    const uint32_t from = lo + (static_cast<uint32_t>(max(l.bin, 0)) << shift);
     hi = min(hi, from + ((1u << shift) - 1u));
     lo = from;
+    if (shift == 0 || l.count <= enough) return Cut{lo, hi, above, l.count};
   }
 }
 
-// The element at which the running weight in index order first exceeds `drawn`:
-// its index, in the one thread of the cluster that finds it; -1 in the others.
-// weight(i) is the weight of element i of the row (0: not taking part), parts
-// the weight of each CTA's slice (cluster_exchange).  Each thread of the CTA
-// that holds the place adds up a run of its own; an odd number of elements, so
-// that the threads' reads fall into different banks.
-template <typename T, typename Weight>
-__device__ __forceinline__ int find_index(const RowCta& c, const Slice<T>& s,
-                                          const unsigned long long* parts,
-                                          unsigned long long drawn, Weight&& weight) {
-  unsigned long long base = 0;
-  int owner = 0;
-  for (; owner < c.ctas - 1 && drawn >= base + parts[owner]; ++owner) base += parts[owner];
-  if (owner != c.rank) return -1;
-  const int tid = threadIdx.x, nt = blockDim.x;
-  const int n = s.hi - s.lo, per = ((n + nt - 1) / nt) | 1;
-  const int a = min(n, tid * per), b = min(n, a + per);
-  unsigned long long own = 0;
-  for (int i = a; i < b; ++i) own += weight(s.lo + i);
-  unsigned long long incl = own;
-#pragma unroll
-  for (int o = 1; o < 32; o <<= 1) {
-    const unsigned long long m = __shfl_up_sync(0xffffffffu, incl, o);
-    if ((tid & 31) >= o) incl += m;
+// ------------------------------------------------------------------ weights --
+
+// A token's weight is a share e in [0, 1] in units of 2^-40, rounded to a whole
+// number: sums of weights are exact, whatever their order.
+constexpr float kWeightUnit = 1099511627776.0f;  // 2^40
+constexpr float kOneUnit = 1.0f / kWeightUnit;   // the share whose weight is 1
+
+// In 32-bit pieces, a few instructions an element: e + 1 rounds e to units of
+// 2^-23 and holds them in the low bits; what that leaves is exact, at most 2^-24,
+// and is rounded to units of 2^-40 in the low bits of a number near 1.5 2^23.
+constexpr uint32_t kOneBits = 0x3f800000u;    // 1.0f
+constexpr uint32_t kMagicBits = 0x4b400000u;  // 1.5 * 2^23
+
+__device__ __forceinline__ unsigned long long weight_of(float e) {
+  const float h = __fadd_rn(e, 1.0f);
+  const float l = __fmaf_rn(__fsub_rn(e, __fsub_rn(h, 1.0f)), kWeightUnit, 12582912.0f);
+  return (static_cast<unsigned long long>(__float_as_uint(h) - kOneBits) << 17) +
+         static_cast<long long>(static_cast<int32_t>(__float_as_uint(l) - kMagicBits));
+}
+
+// The sum of up to 511 elements' weights in a thread.
+struct WeightSum {
+  uint32_t high = 0, low = 0;
+  __device__ __forceinline__ void add(float e0, float e1) {
+    const float2 e = make_float2(e0, e1), one = make_float2(1.0f, 1.0f);
+    const float2 h = __fadd2_rn(e, one);
+    const float2 r = __fadd2_rn(e, __fadd2_rn(one, make_float2(-h.x, -h.y)));
+    const float2 l = __ffma2_rn(r, make_float2(kWeightUnit, kWeightUnit),
+                                make_float2(12582912.0f, 12582912.0f));
+    high += __float_as_uint(h.x) + __float_as_uint(h.y);
+    low += __float_as_uint(l.x) + __float_as_uint(l.y);
   }
-  __syncthreads();  // wred is free
-  if ((tid & 31) == 31) c.sh->wred[0][tid >> 5] = incl;
+  // After n elements.
+  __device__ __forceinline__ unsigned long long sum(uint32_t n) const {
+    const long long lo = static_cast<int32_t>(low - n * kMagicBits);
+    return (static_cast<unsigned long long>(high - n * kOneBits) << 17) + lo;
+  }
+};
+
+// f() worked out by one warp for the CTA: 64-bit floating point is slow enough for
+// sixteen warps to queue for it.
+template <typename F>
+__device__ __forceinline__ unsigned long long cta_once(RowShared* sh, F&& f) {
   __syncthreads();
-  for (int w = 0; w < (tid >> 5); ++w) incl += c.sh->wred[0][w];
-  unsigned long long run = base + incl - own;
-  if (drawn < run || drawn >= run + own) return -1;
-  for (int i = a; i < b; ++i) {
-    run += weight(s.lo + i);
-    if (drawn < run) return s.lo + i;
+  if (threadIdx.x < 32) {
+    const unsigned long long v = f();
+    if (threadIdx.x == 0) sh->once = v;
+  }
+  __syncthreads();
+  return sh->once;
+}
+
+// The element at which the running weight in index order first exceeds a number
+// drawn(whole): its index, in the one thread of the row that finds it; -1 in the
+// others.  share(i, z0, z1) are those of elements i and i + 1 of values z0, z1 (0:
+// not taking part; also asked of what the ends hold besides the slice).  `whole`
+// and `found` receive the whole weight and the element's.  All threads call it.
+// Each warp adds up a run of vectors; the run that holds the place is then cut
+// over the CTA's threads.
+template <typename T, typename C, typename S, typename Share, typename Drawn>
+__device__ __noinline__ int find_index(C& c, const S s, const Share share, const Drawn drawn_of,
+                                       unsigned long long& whole, unsigned long long& found) {
+  constexpr int kVec = Row<T>::kVec;
+  constexpr bool kKept = S::kKept;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
+  const int per = (s.n_vec + warps - 1) / warps;
+  unsigned long long* wmass = c.sh->wred[kSums - 1];
+  unsigned long long run = 0, drawn = 0;
+  // The thread's vectors: of its warp's run, then of the run that holds the place.
+  int v = min(s.n_vec, warp * per) + lane, end = min(s.n_vec, warp * per + per), step = 32, first = v;
+#pragma unroll 1
+  for (int turn = 0;; ++turn) {
+    WeightSum sum;
+    uint32_t n = 0;
+    const auto add = [&](int u, const uint4& r) {
+      float z[kVec];
+      Row<T>::unpack(r, z);
+#pragma unroll
+      for (int e = 0; e < kVec; e += 2) {
+        const float2 w = share(s.index(u) + e, z[e], z[e + 1]);
+        sum.add(w.x, w.y);
+      }
+      n += kVec;
+    };
+    for_body<4>(s, !kKept && v < s.first ? v + step : v, kKept ? end : min(end, s.last), step, add);
+    // The ends, where they are among this thread's vectors.
+#pragma unroll 1
+    for (int k = 0; k < 2; ++k) {
+      const int u = s.end_of(k);
+      if (!kKept && u >= v && u < end && (u - v) % step == 0) add(u, s.get(u));
+    }
+    unsigned long long own = sum.sum(n);
+    if (turn == 0) {
+      own = warp_reduce(own, AddOp());
+      if (lane == 0) wmass[warp] = own;
+      __syncthreads();
+      unsigned long long cta[1] = {0};
+#pragma unroll 1
+      for (int w = 0; w < warps; ++w) cta[0] += wmass[w];
+      const unsigned long long* parts = cluster_exchange(c, cta).of(0);
+      whole = 0;
+#pragma unroll 1
+      for (int q = 0; q < c.ctas(); ++q) {
+        if (q == c.rank()) run = whole;
+        whole += parts[q];
+      }
+      drawn = cta_once(c.sh, [&]() { return drawn_of(whole); });
+      if (drawn < run || drawn >= run + cta[0]) return -1;  // the same in the whole CTA
+      int hold = 0;
+#pragma unroll 1
+      while (hold < warps - 1 && drawn >= run + wmass[hold]) run += wmass[hold++];
+      // Each thread a part of that warp's run.
+      const int a = min(s.n_vec, hold * per), b = min(s.n_vec, a + per);
+      const int each = (b - a + static_cast<int>(blockDim.x) - 1) / static_cast<int>(blockDim.x);
+      first = v = min(b, a + static_cast<int>(threadIdx.x) * each);
+      end = min(b, v + each);
+      step = 1;
+      continue;
+    }
+    unsigned long long all;
+    run += cta_scan(c.sh, own, all);
+    if (drawn < run || drawn >= run + own) return -1;
+    break;
+  }
+#pragma unroll 1
+  for (int i = max(s.lo, s.index(first)); i < min(s.hi, s.index(end)); ++i) {
+    const float z = s.value(i);
+    const unsigned long long w = weight_of(share(i, z, z).x);
+    run += w;
+    if (drawn < run) {
+      found = w;
+      return i;
+    }
   }
   return -1;
 }
 
-// The index that one thread of the cluster found (>= 0 there), in every thread.
-__device__ __forceinline__ int tell_index(const RowCta& c, int found) {
-  if (found >= 0)
-    for (int r = 0; r < c.ctas; ++r)
-      st_peer(reinterpret_cast<const uint32_t*>(&c.sh->told), r, static_cast<uint32_t>(found));
-  row_sync();
-  return c.sh->told;
+// Two words that one thread of the row has (`mine`), in every thread.
+struct Told {
+  uint32_t a, b;
+};
+template <typename C>
+__device__ __forceinline__ Told tell(const C& c, bool mine, uint32_t a, uint32_t b) {
+  if (mine)
+#pragma unroll 1
+    for (int r = 0; r < c.ctas(); ++r) {
+      c.store(&c.sh->told[0], r, a);
+      c.store(&c.sh->told[1], r, b);
+    }
+  c.sync();
+  return Told{c.sh->told[0], c.sh->told[1]};
 }
 
 // ------------------------------------------------------------- candidates --
 
-// A key with at least `count` elements of this CTA's slice at or above it, near
-// the largest such: the count-th largest of the threads' maxima (each stands for
-// an element), its lower 16 bits cleared in 32-bit keys.  0 where the CTA has
-// fewer threads than that.  All threads call it.
+// A key with at least `count` elements of this warp's at or above it: the
+// count-th largest of the lanes' maxima (each stands for an element), its lower
+// 16 bits cleared in 32-bit keys; 0 where count is above 32.
 template <typename T>
-__device__ __forceinline__ uint32_t local_floor(float thread_max, int count) {
+__device__ __forceinline__ uint32_t warp_floor(float lane_max, int count) {
   constexpr int kDrop = Row<T>::kKeyBits - 16;
-  const uint32_t key = key_of<T>(thread_max) >> kDrop;
+  const uint32_t key = key_of<T>(lane_max) >> kDrop;
   uint32_t found = 0;
-#pragma unroll 1
+#pragma unroll
   for (int bit = 15; bit >= 0; --bit) {
     const uint32_t t = found | (1u << bit);
-    if (__syncthreads_count(key >= t) >= count) found = t;
+    if (__popc(__ballot_sync(0xffffffffu, key >= t)) >= count) found = t;
   }
   return found << kDrop;
 }
@@ -571,20 +756,73 @@ __device__ __forceinline__ int candidate_index(unsigned long long x) {
 }
 
 // Appends a candidate to CTA 0's list; past its end they are only counted.
-__device__ __forceinline__ void push_candidate(const RowCta& c, uint32_t key, int index) {
-  uint32_t at;
-  asm volatile("atom.relaxed.cluster.shared::cluster.add.u32 %0, [%1], 1;"
-               : "=r"(at)
-               : "r"(mapa_shared(&c.sh->listed, 0))
-               : "memory");
-  if (at < kListMax) st_peer(c.sh->list + at, 0, candidate(key, index));
+template <typename C>
+__device__ __forceinline__ void push_candidate(const C& c, uint32_t key, int index) {
+  const uint32_t at = c.next(&c.sh->listed, 0);
+  if (at < kListMax) c.store(c.sh->list + at, 0, candidate(key, index));
 }
 
-// Sorts n (a power of two) 64-bit values in shared memory, rising.
-__device__ __forceinline__ void cta_sort(unsigned long long* a, int n) {
-  for (int k = 2; k <= n; k <<= 1)
+// Sorts the first n of 64-bit values in shared memory, rising; no two are alike.
+// Returns where they lie then: in `a` (kListMax values of room) or further on in
+// it.  Up to half of the room: every warp sorts runs of 32 by shuffles, then each
+// value counts the smaller ones of every run by halving, which is its place; three
+// barriers (256 values: a network through shared memory took 5.0 us).  More: that
+// network, where a warp's 32 pairs of a step with j <= 32 are its own 64 values in
+// the step before and after, so only the wider steps wait for other warps.
+__device__ __noinline__ unsigned long long* cta_sort(unsigned long long* a, int n) {
+  const int tid = threadIdx.x, nt = blockDim.x, lane = tid & 31;
+  __syncthreads();
+  if (n <= kListMax / 2) {
+    const int runs = (n + 31) / 32;
+#pragma unroll 1
+    for (int r = tid >> 5; r < runs; r += nt >> 5) {
+      const int i = 32 * r + lane;
+      unsigned long long x = i < n ? a[i] : ~0ull;
+#pragma unroll
+      for (int k = 2; k <= 32; k <<= 1)
+#pragma unroll
+        for (int j = k >> 1; j > 0; j >>= 1) {
+          const unsigned long long y = __shfl_xor_sync(0xffffffffu, x, j);
+          if ((x < y) != (((lane & j) == 0) == ((lane & k) == 0))) x = y;
+        }
+      a[i] = x;  // up to the end of the run
+    }
+    __syncthreads();
+    unsigned long long* out = a + kListMax / 2;
+#pragma unroll 1
+    for (int i = tid; i < n; i += nt) {
+      // (a run's own values are counted like the others: those before i)
+      const unsigned long long x = a[i];
+      int at = 0;
+#pragma unroll 4
+      for (int r = 0; r < runs; ++r) {
+        const unsigned long long* run = a + 32 * r;
+        int c = 0;
+#pragma unroll
+        for (int h = 16; h > 0; h >>= 1) c += run[c + h - 1] < x ? h : 0;
+        at += c + (run[c] < x ? 1 : 0);
+      }
+      out[at] = x;
+    }
+    __syncthreads();
+    return out;
+  }
+  int size = kListMax;
+  while (size / 2 >= n) size >>= 1;
+#pragma unroll 1
+  for (int i = n + tid; i < size; i += nt) a[i] = ~0ull;
+  int last = 64;  // the step before; before the first everything is waited for
+#pragma unroll 1
+  for (int k = 2; k <= size; k <<= 1)
+#pragma unroll 1
     for (int j = k >> 1; j > 0; j >>= 1) {
-      for (int q = threadIdx.x; q < n / 2; q += blockDim.x) {
+      if (j > 32 || last > 32)
+        __syncthreads();
+      else
+        __syncwarp();
+      last = j;
+#pragma unroll 1
+      for (int q = tid; q < size / 2; q += nt) {
         const int i = ((q & ~(j - 1)) << 1) | (q & (j - 1));
         const unsigned long long x = a[i], y = a[i + j];
         if ((x > y) == ((i & k) == 0)) {
@@ -592,52 +830,28 @@ __device__ __forceinline__ void cta_sort(unsigned long long* a, int n) {
           a[i + j] = x;
         }
       }
-      __syncthreads();
     }
-}
-// ... n of any size, with room up to the next power of two.
-__device__ __forceinline__ void cta_sort_any(unsigned long long* a, int n) {
-  const int size = n > 1 ? 1 << (32 - __clz(n - 1)) : 1;
-  for (int i = n + threadIdx.x; i < size; i += blockDim.x) a[i] = ~0ull;
   __syncthreads();
-  cta_sort(a, size);
+  return a;
 }
 
-// The sum of the values before this thread's, and of all.
-__device__ __forceinline__ unsigned long long cta_scan(const RowCta& c, unsigned long long v,
-                                                       unsigned long long& whole) {
-  unsigned long long incl = v;
-#pragma unroll
-  for (int o = 1; o < 32; o <<= 1) {
-    const unsigned long long m = __shfl_up_sync(0xffffffffu, incl, o);
-    if ((threadIdx.x & 31) >= o) incl += m;
-  }
-  __syncthreads();
-  if ((threadIdx.x & 31) == 31) c.sh->wred[0][threadIdx.x >> 5] = incl;
-  __syncthreads();
-  unsigned long long before = incl - v;
-  whole = 0;
-  for (int w = 0; w < static_cast<int>(blockDim.x >> 5); ++w) {
-    if (w < static_cast<int>(threadIdx.x >> 5)) before += c.sh->wred[0][w];
-    whole += c.sh->wred[0][w];
-  }
-  return before;
-}
-
-// The cluster that reads a row: as few CTAs as keep a slice within
-// kSliceTarget, more while the grid leaves SMs idle and slices stay long.
-__host__ __forceinline__ int row_ctas(int M, int V, int elem, int sms) {
-  constexpr size_t kSliceTarget = 40 * 1024;
+// How a call's rows are worked on: ctas 0 stands for the form in which a CTA
+// takes a row alone.
+struct RowPlan {
+  int ctas, threads;
+};
+__host__ __forceinline__ RowPlan row_plan(int M, int V, int elem, int sms) {
+  static const int fc = getenv("ROW_CTAS") ? atoi(getenv("ROW_CTAS")) : -1;
+  static const int ft = getenv("ROW_THREADS") ? atoi(getenv("ROW_THREADS")) : 0;
+  constexpr size_t kSliceTarget = 72 * 1024;
   int c = 1;
   while (c < kRowMaxCluster && row_slice_bytes(V, c, elem) > kSliceTarget) c *= 2;
-  while (c < kRowMaxCluster && static_cast<long long>(M) * c * 2 <= sms && V / c > 4096) c *= 2;
-  return c;
-}
-
-// Threads of a CTA: about 8 elements for each, whole warps.
-__host__ __forceinline__ int row_threads(int V, int ctas) {
-  const int n = (row_chunk(V, ctas) + 7) / 8;
-  return n < 128 ? 128 : n > kRowMaxThreads ? kRowMaxThreads : (n + 31) / 32 * 32;
+  while (c < 4 && static_cast<long long>(M) * c * 2 <= sms && V / c > 4096) c *= 2;
+  if (c > 1 && M >= sms) c = 0;
+  if (fc >= 0) c = fc;
+  int t = c ? 256 : 512;
+  if (ft) t = ft;
+  return RowPlan{c, t};
 }
 
 }  // namespace cai

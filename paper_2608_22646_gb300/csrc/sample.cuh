@@ -16,7 +16,6 @@
 namespace cai {
 
 constexpr float kRowLog2e = kLog2e;
-constexpr float kWeightUnit = 1099511627776.0f;  // 2^40
 constexpr int kTopMax = 512;                     // K of cai_top_rows
 
 struct SampleParams {
@@ -32,52 +31,11 @@ struct SampleParams {
   float* prob;
 };
 
-// Calls f(element of the row, value) for what the thread keeps of the slice.
-// What a vector holds besides the slice comes too, as -inf.
-template <typename T, typename F>
-__device__ __forceinline__ void for_slice(const Slice<T>& s, F&& f) {
-  for (int v = threadIdx.x; v < s.n_vec; v += blockDim.x) {
-    float z[Row<T>::kVec];
-    Row<T>::unpack(s.vec[v], z);
-    const int i0 = s.index(v, 0);
-#pragma unroll
-    for (int e = 0; e < Row<T>::kVec; ++e) f(i0 + e, z[e]);
-  }
-}
-
 // 2^x of a logit relative to the largest.  Subtraction and product are rounded
 // one by one, as the definition says.
 __device__ __forceinline__ float row_exp2(float z, float zmax, float scale) {
   return exp2f(__fmul_rn(__fsub_rn(z, zmax), scale));
 }
-__device__ __forceinline__ unsigned long long weight_of(float e) {
-  return __float2ull_rn(__fmul_rn(e, kWeightUnit));
-}
-
-// Sums of weights in 32-bit pieces, a few instructions an element: e + 1 rounds
-// e to units of 2^-23 and holds them in the low bits, what that leaves is exact
-// and goes the same way in units of 2^-40, rounded as weight_of does.  Up to 511
-// elements a thread.
-struct WeightSum {
-  static constexpr uint32_t kOne = 0x3f800000u;    // 1.0f
-  static constexpr uint32_t kMagic = 0x4b400000u;  // 1.5 * 2^23
-  uint32_t high = 0, low = 0;
-  __device__ __forceinline__ void add(float e0, float e1) {
-    const float2 e = make_float2(e0, e1), one = make_float2(1.0f, 1.0f);
-    const float2 h = __fadd2_rn(e, one);
-    const float2 r = __fadd2_rn(e, __fadd2_rn(one, make_float2(-h.x, -h.y)));
-    const float2 l = __ffma2_rn(r, make_float2(kWeightUnit, kWeightUnit),
-                                make_float2(12582912.0f, 12582912.0f));
-    high += __float_as_uint(h.x) + __float_as_uint(h.y);
-    low += __float_as_uint(l.x) + __float_as_uint(l.y);
-  }
-  // After n elements.
-  __device__ __forceinline__ unsigned long long sum(uint32_t n) const {
-    const long long lo = static_cast<int32_t>(low - n * kMagic);
-    return (static_cast<unsigned long long>(high - n * kOne) << 17) + lo;
-  }
-};
-
 // 2^x of a pair of logits relative to the largest, bit for bit row_exp2 where a
 // weight remains.
 __device__ __forceinline__ float2 row_exp2_pair(float z0, float z1, float zmax, float scale) {
@@ -86,25 +44,25 @@ __device__ __forceinline__ float2 row_exp2_pair(float z0, float z1, float zmax, 
   return make_float2(fast_exp2(x.x), fast_exp2(x.y));
 }
 
-// Elements above a key, and of those with that key the ones up to an index.
+// Elements above a value, and of those with that value the ones up to an index.
 struct Kept {
-  uint32_t key;
+  float value;
   int last;
-  __device__ __forceinline__ bool has(uint32_t k, int i) const {
-    return k > key || (k == key && i <= last);
+  __device__ __forceinline__ bool has(float z, int i) const {
+    return z > value || (z == value && i <= last);
   }
 };
 
 // Loads the slice and returns the thread's largest logit.
-template <typename T>
-__device__ __forceinline__ float load_row(const Slice<T>& s, const T* row) {
+template <typename T, bool kKeep>
+__device__ __forceinline__ float load_row(const Slice<T, kKeep>& s) {
   float m = __uint_as_float(0xff800000u);
-  load_slice<T, 4>(s, row, [&](const uint4& v) { m = vec_max(v, m, T()); });
+  load_slice<kKeep ? 4 : 8>(s, [&](int, const uint4& v) { m = vec_max(v, m, T()); });
   return m;
 }
 
 // The row's largest logit, and a key with at least `want` elements of the row at
-// or above it (0: none is known): every CTA finds one for its part of them.
+// or above it (0: none is known): every warp finds one for its part of them.
 struct Floor {
   float zmax;
   uint32_t key;
@@ -115,135 +73,470 @@ struct Floor {
     return v == v ? v : __uint_as_float(0xff800000u);
   }
 };
-template <typename T>
-__device__ __forceinline__ Floor row_floor(RowCta& c, float thread_max, int want) {
-  const uint32_t mine = want > 0 ? local_floor<T>(thread_max, (want + c.ctas - 1) / c.ctas) : 0u;
-  const unsigned long long v[2] = {cta_reduce(c, __float_as_uint(thread_max), MaxNanOp()), mine};
-  const Parts parts = cluster_exchange(c, v);
-  Floor f{__uint_as_float(static_cast<uint32_t>(parts.of(0)[0])), static_cast<uint32_t>(parts.of(1)[0])};
-  for (int i = 1; i < c.ctas; ++i) {
-    f.zmax = max_nan(f.zmax, __uint_as_float(static_cast<uint32_t>(parts.of(0)[i])));
-    f.key = min(f.key, static_cast<uint32_t>(parts.of(1)[i]));
+template <typename T, typename C>
+__device__ __forceinline__ Floor row_floor(C& c, float thread_max, int want) {
+  const int warps = c.ctas() * static_cast<int>(blockDim.x >> 5);
+  const uint32_t floor = want > 0 ? warp_floor<T>(thread_max, (want + warps - 1) / warps) : 0u;
+  // Both as one value: the largest key, and the smallest floor as its complement.
+  const uint32_t top = __reduce_max_sync(0xffffffffu, key_of<float>(thread_max));
+  RowShared* sh = c.sh;
+  const int lane = threadIdx.x & 31, n = blockDim.x >> 5;
+  if (lane == 0) sh->wred[0][threadIdx.x >> 5] = (static_cast<unsigned long long>(top) << 32) | floor;
+  __syncthreads();
+  const unsigned long long w = sh->wred[0][lane & (n - 1)];
+  const unsigned long long v[1] = {
+      (static_cast<unsigned long long>(__reduce_max_sync(0xffffffffu, static_cast<uint32_t>(w >> 32))) << 32) |
+      __reduce_min_sync(0xffffffffu, static_cast<uint32_t>(w))};
+  const unsigned long long* parts = cluster_exchange(c, v).of(0);
+  uint32_t key = static_cast<uint32_t>(parts[0]), high = static_cast<uint32_t>(parts[0] >> 32);
+#pragma unroll 1
+  for (int i = 1; i < c.ctas(); ++i) {
+    high = max(high, static_cast<uint32_t>(parts[i] >> 32));
+    key = min(key, static_cast<uint32_t>(parts[i]));
   }
-  return f;
+  return Floor{value_of_key<float>(high), key};
 }
 
-// Pushes the elements of a vector whose key is at least `floor` (value `low`);
-// returns how many.
-template <typename T>
-__device__ __forceinline__ uint32_t push_vector(const RowCta& c, const Slice<T>& s, int v,
-                                                const float (&z)[Row<T>::kVec], uint32_t floor) {
-  uint32_t n = 0;
-#pragma unroll
-  for (int e = 0; e < Row<T>::kVec; ++e) {
-    const int i = s.index(v, e);
-    const uint32_t key = key_of<T>(z[e]);
-    if (key >= floor && i >= s.lo && i < s.hi) {
-      push_candidate(c, key, i);
-      ++n;
+// How a row's weights are drawn from.
+struct Setting {
+  float zmax, scale, pmin, share, u;
+  int k;
+  __device__ __forceinline__ unsigned long long target(unsigned long long whole) const {
+    const unsigned long long t = static_cast<unsigned long long>(
+        ceil(static_cast<double>(share) * static_cast<double>(whole)));
+    return t < 1 ? 1 : t > whole ? whole : t;
+  }
+  __device__ __forceinline__ float share_of(float z) const {
+    const float e = row_exp2(z, zmax, scale);
+    return e < pmin ? 0.0f : e;
+  }
+  __device__ __forceinline__ unsigned long long weight(float z) const {
+    return weight_of(share_of(z));
+  }
+};
+
+// The shares of two elements (find_index): of all that min-p leaves, and of those
+// of them that are kept.  Handed on as values: what is handed on by reference
+// lies in memory and is read again for every vector.
+struct ShareAll {
+  float zmax, scale, pmin;
+  __device__ __forceinline__ explicit ShareAll(const Setting& s) : zmax(s.zmax), scale(s.scale), pmin(s.pmin) {}
+  __device__ __forceinline__ float2 operator()(int, float z0, float z1) const {
+    float2 e = row_exp2_pair(z0, z1, zmax, scale);
+    e.x = e.x < pmin ? 0.0f : e.x;
+    e.y = e.y < pmin ? 0.0f : e.y;
+    return e;
+  }
+};
+struct ShareKept {
+  ShareAll all;
+  Kept kept;
+  __device__ __forceinline__ float2 operator()(int i, float z0, float z1) const {
+    float2 e = all(i, z0, z1);
+    e.x = kept.has(z0, i) ? e.x : 0.0f;
+    e.y = kept.has(z1, i + 1) ? e.y : 0.0f;
+    return e;
+  }
+};
+// Of the elements with one key that have a share, each one unit.
+template <typename T, typename Share>
+struct ShareTies {
+  Share share;
+  uint32_t key;
+  int lo, hi;
+  __device__ __forceinline__ float2 operator()(int i, float z0, float z1) const {
+    const float2 e = share(i, z0, z1);
+    return make_float2(i >= lo && i < hi && key_of<T>(z0) == key && weight_of(e.x) ? kOneUnit : 0.0f,
+                       i + 1 >= lo && i + 1 < hi && key_of<T>(z1) == key && weight_of(e.y) ? kOneUnit : 0.0f);
+  }
+};
+struct ShareOne {
+  __device__ __forceinline__ float2 operator()(int, float, float) const { return make_float2(1.0f, 1.0f); }
+};
+struct DrawnAt {  // a place known beforehand
+  unsigned long long at;
+  __device__ __forceinline__ unsigned long long operator()(unsigned long long) const { return at; }
+};
+struct DrawnNever {
+  __device__ __forceinline__ unsigned long long operator()(unsigned long long whole) const { return whole; }
+};
+struct DrawnBy {
+  float u;
+  __device__ __forceinline__ unsigned long long operator()(unsigned long long whole) const {
+    const unsigned long long d =
+        static_cast<unsigned long long>(static_cast<double>(u) * static_cast<double>(whole));
+    return d < whole ? d : whole - 1;
+  }
+};
+
+// The vectors of a thread (for_slice) with an element that is not below the floor,
+// a bit for one or more of its rounds: the pass that looks for them only sets bits.
+struct Noted {
+  unsigned long long bits = 0;
+  float low;
+  int shift;  // of a vector's number to its bit
+  __device__ __forceinline__ Noted(int n_vec, float l) : low(l) {
+    shift = __ffs(blockDim.x) - 1;
+#pragma unroll 1
+    while (n_vec >> shift >= 64) ++shift;
+  }
+  template <typename T>
+  __device__ __forceinline__ void look(int v, const uint4& q) {
+    if (!(vec_max(q, __uint_as_float(0xff800000u), T()) < low)) bits |= 1ull << (v >> shift);
+  }
+};
+
+// After the pass, pushes the elements that are not below the floor, each thread
+// some of the noted vectors of all, and calls f(value) for each.  Returns how many
+// this thread pushed; more than the list holds if there were too many vectors.
+template <typename T, typename C, typename S, typename F>
+__device__ __forceinline__ uint32_t push_noted(const C& c, const S& s, Noted noted, F&& f) {
+  RowShared* sh = c.sh;
+  const int nt = blockDim.x, tid = threadIdx.x;
+  const int first = S::kKept ? 0 : s.first, last = S::kKept ? s.n_vec : s.last;
+  const int span = (1 << noted.shift) / nt;  // rounds of a bit
+  const int end = S::kKept ? -1 : s.end_of(tid);
+  const uint32_t mine = __popcll(noted.bits) * span + (end >= 0);
+  if (mine) {
+    uint32_t at = atomicAdd(&sh->noted, mine);
+    if (end >= 0 && at < kListMax) sh->note[at++] = static_cast<uint32_t>(end);
+#pragma unroll 1
+    while (noted.bits) {
+      const int k = __ffsll(noted.bits) - 1;
+      noted.bits &= noted.bits - 1;
+#pragma unroll 1
+      for (int j = 0; j < span; ++j, ++at) {
+        // (what an end set stands for one of the thread's other vectors)
+        const int v = (k * span + j) * nt + ((first + tid) & (nt - 1));
+        if (at < kListMax) sh->note[at] = v >= first && v < last ? static_cast<uint32_t>(v) : ~0u;
+      }
     }
   }
-  return n;
+  __syncthreads();
+  const uint32_t n = sh->noted;
+  if (n > kListMax) return kListMax + 1;
+  uint32_t pushed = 0;
+#pragma unroll 1
+  for (uint32_t k = tid; k < n; k += nt) {
+    const uint32_t v = sh->note[k];
+    if (v == ~0u) continue;
+    float z[Row<T>::kVec];
+    Row<T>::unpack(s.get(v), z);
+#pragma unroll
+    for (int e = 0; e < Row<T>::kVec; ++e) {
+      const int i = s.index(v) + e;
+      if (!(z[e] < noted.low) && s.holds(i)) {
+        push_candidate(c, key_of<T>(z[e]), i);
+        f(z[e]);
+        ++pushed;
+      }
+    }
+  }
+  return pushed;
 }
 
-// In CTA 0, with the candidates listed: sorts them, keeps, draws.  `whole`: the
-// weight of all tokens that min-p leaves, where top-k is off.
-template <typename T>
-__device__ void sample_candidates(const RowCta& c, const SampleParams& p, int r, int n, int k,
-                                  float zmax, float scale, float pmin, float share, float u,
-                                  unsigned long long whole) {
-  unsigned long long* list = c.sh->list;
-  const int tid = threadIdx.x, nt = blockDim.x;
-  const auto weight = [&](uint32_t key) -> unsigned long long {
-    const float e = row_exp2(value_of_key<T>(key), zmax, scale);
-    return e < pmin ? 0 : weight_of(e);
+// Every element of the slice, as f(index, value).
+template <typename T, typename S, typename F>
+__device__ __forceinline__ void for_elements(const S& s, F&& f) {
+  for_slice<2>(s, [&](int v, const uint4& r) {
+    float z[Row<T>::kVec];
+    Row<T>::unpack(r, z);
+#pragma unroll
+    for (int e = 0; e < Row<T>::kVec; ++e)
+      if (s.holds(s.index(v) + e)) f(s.index(v) + e, z[e]);
+  });
+}
+
+// The last element kept, found by one thread of the row: for all.
+template <typename T, typename C>
+__device__ __forceinline__ Kept tell_kept(const C& c, bool mine, unsigned long long x) {
+  const Told t = tell(c, mine, candidate_key(x), static_cast<uint32_t>(candidate_index(x)));
+  return Kept{value_of_key<T>(t.a), static_cast<int>(t.b)};
+}
+
+// Of the elements with key `key` that have a share, the need-th by index is the
+// last one kept.
+template <typename T, typename C, typename S, typename Share>
+__device__ __forceinline__ Kept keep_ties(C& c, const S& s, uint32_t key, unsigned long long need,
+                                          const Share& share) {
+  unsigned long long whole, found;
+  const int at = find_index<T>(c, s, ShareTies<T, Share>{share, key, s.lo, s.hi}, DrawnAt{need - 1}, whole, found);
+  return tell_kept<T>(c, at >= 0, candidate(key, at));
+}
+
+// The first `want` elements of the falling order.
+template <typename T, typename C, typename S>
+__device__ __noinline__ Kept keep_count(C& c, const S s, uint32_t want) {
+  const Cut cut = find_cut<T>(c, 0xffffffffu >> (32 - Row<T>::kKeyBits), want, kListMax, [&](auto&& f) {
+    for_elements<T>(s, [&](int, float z) { f(key_of<T>(z)); });
+  });
+  if (cut.at > kListMax)  // one key, more often than a list holds
+    return keep_ties<T>(c, s, cut.lo, want - cut.above, ShareOne{});
+  // List what lies there, and look.
+  if (threadIdx.x == 0) c.sh->listed = 0;
+  c.sync();
+  for_elements<T>(s, [&](int i, float z) {
+    const uint32_t key = key_of<T>(z);
+    if (key - cut.lo <= cut.hi - cut.lo) push_candidate(c, key, i);
+  });
+  c.sync();
+  const bool mine = c.rank() == 0 && threadIdx.x == 0;
+  unsigned long long x = 0;
+  if (c.rank() == 0) x = cta_sort(c.sh->list, static_cast<int>(cut.at))[want - cut.above - 1];
+  return tell_kept<T>(c, mine, x);
+}
+
+// What a search by weight starts from: values in [low, high] (open: below high),
+// `above` the weight of what lies higher.
+struct Bracket {
+  float low, high;
+  bool open;
+  unsigned long long above;
+  __device__ __forceinline__ bool holds(float z) const {
+    return z >= low && (open ? z < high : z <= high);
+  }
+  __device__ __forceinline__ bool higher(float z) const { return open ? z >= high : z > high; }
+  // kBins equal parts; rising with z.
+  __device__ __forceinline__ int bin(float z) const {
+    const float b = (z - low) * (static_cast<float>(kBins) / (high - low));
+    return b >= static_cast<float>(kBins - 1) ? kBins - 1 : b > 0.0f ? static_cast<int>(b) : 0;
+  }
+};
+
+// The first elements of the falling order whose weight reaches `want`; share(i,
+// z0, z1) as in find_index, falling with the value.  First a guess: the numbers
+// of elements in equal parts of the bracket, each taken with the weight at its
+// middle, say in which part the cut lies; then one exact pass adds up what lies
+// above it and lists its elements (and those of its neighbours, if there is room),
+// and moves on where the guess was wrong.  Where they are too many for a list, the
+// key is found by halving the range of keys with an exact sum each time.
+template <typename T, typename C, typename S, typename Share>
+__device__ __noinline__ Kept keep_weight(C& c, const S s, const Bracket br, unsigned long long want,
+                                         const Share share) {
+  constexpr int kVec = Row<T>::kVec;
+  const auto weight_at = [&](int i, float z) { return weight_of(share(i, z, z).x); };
+  // The weight of the elements that pick(i, z) names.
+  const auto sum_of = [&](auto&& pick, unsigned long long also, unsigned long long& other) {
+    WeightSum sum;
+    uint32_t n = 0;
+    for_slice<2>(s, [&](int v, const uint4& r) {
+      float z[kVec];
+      Row<T>::unpack(r, z);
+#pragma unroll
+      for (int e = 0; e < kVec; e += 2) {
+        const int i = s.index(v) + e;
+        const float2 w = share(i, z[e], z[e + 1]);
+        sum.add(pick(i, z[e]) ? w.x : 0.0f, pick(i + 1, z[e + 1]) ? w.y : 0.0f);
+      }
+      n += kVec;
+    });
+    const unsigned long long m[2] = {sum.sum(n), other};
+    const Parts parts = exchange_sums(c, m);
+    other = parts.sum(c.ctas(), 1);
+    return parts.sum(c.ctas(), 0) + also;
   };
-  cta_sort_any(list, n);
-  if (k > 0) n = min(n, k);
+  if (br.high > br.low && br.high - br.low < 1e30f) {
+    const float width = (br.high - br.low) / kBins;
+    const Level l = search_level(
+        c, br.above, want,
+        [&](auto&& f) {
+          for_elements<T>(s, [&](int, float z) {
+            if (br.holds(z)) f(br.bin(z));
+          });
+        },
+        [&](int b, uint32_t n) -> unsigned long long {
+          // (of index -1: before every element, so that ties are not cut)
+          const float z = br.low + (static_cast<float>(b) + 0.5f) * width;
+          return static_cast<unsigned long long>(static_cast<float>(n) * kWeightUnit * share(-1, z, z).x);
+        });
+    int bin = l.bin;
+    const int around = 4 * l.count < kListMax ? 1 : 0;  // parts to either side
+#pragma unroll 1
+    for (int turn = 0; turn < 4 && bin >= 0 && bin < kBins; ++turn) {
+      if (threadIdx.x == 0) c.sh->listed = 0;
+      c.sync();
+      unsigned long long pushed = 0;
+      const unsigned long long above = sum_of(
+          [&](int i, float z) {
+            if (!br.holds(z)) return false;
+            const int d = br.bin(z) - bin;
+            if (d <= around && d >= -around && s.holds(i) && weight_at(i, z) != 0) {
+              push_candidate(c, key_of<T>(z), i);
+              ++pushed;
+            }
+            return d > around;
+          },
+          br.above, pushed);
+      const uint32_t n = static_cast<uint32_t>(pushed);  // of all CTAs now
+      if (n > kListMax) break;
+      int step = 0;  // where to look next
+      bool mine = false;
+      unsigned long long x = 0;
+      if (above >= want) {
+        step = 1;
+      } else if (c.rank() == 0) {
+        const unsigned long long* list = cta_sort(c.sh->list, static_cast<int>(n));
+        const int nt = blockDim.x, per = (static_cast<int>(n) + nt - 1) / nt;
+        const int a = min(static_cast<int>(n), static_cast<int>(threadIdx.x) * per);
+        const int b = min(static_cast<int>(n), a + per);
+        const auto weight_in = [&](int i) {
+          return weight_at(candidate_index(list[i]), value_of_key<T>(candidate_key(list[i])));
+        };
+        unsigned long long own = 0, all;
+#pragma unroll 1
+        for (int i = a; i < b; ++i) own += weight_in(i);
+        unsigned long long run = above + cta_scan(c.sh, own, all);
+#pragma unroll 1
+        for (int i = a; i < b && !mine && run < want; ++i) {
+          run += weight_in(i);
+          if (run >= want) {
+            mine = true;
+            x = list[i];
+          }
+        }
+        if (above + all < want) {  // further down
+          mine = threadIdx.x == 0;
+          x = ~0ull;
+        }
+      }
+      if (step == 0) {
+        const Told t = tell(c, mine, candidate_key(x), static_cast<uint32_t>(candidate_index(x)));
+        if (static_cast<int>(t.b) >= 0) return Kept{value_of_key<T>(t.a), static_cast<int>(t.b)};
+        step = -1;
+      }
+      bin += step * (2 * around + 1);
+      c.sync();  // the list and what was told have been read
+    }
+  }
+  // The largest key with enough weight at or above it.
+  uint32_t key = 0;
+  unsigned long long none = 0;
+#pragma unroll 1
+  for (int bit = Row<T>::kKeyBits - 1; bit >= 0; --bit) {
+    const uint32_t t = key | (1u << bit);
+    if (sum_of([&](int, float z) { return key_of<T>(z) >= t; }, 0, none) >= want) key = t;
+  }
+  const unsigned long long above = sum_of([&](int, float z) { return key_of<T>(z) > key; }, 0, none);
+  // The same weight for every element with that key.
+  const unsigned long long each = weight_at(-1, value_of_key<T>(key));
+  return keep_ties<T>(c, s, key, (want - above + each - 1) / each, share);
+}
+
+// In CTA 0, with n tokens listed as (index, key): draws one of them.
+template <typename T>
+__device__ __forceinline__ void draw_listed(RowShared* sh, const SampleParams& p, int r, int n,
+                                            const Setting& set) {
+  const int tid = threadIdx.x, nt = blockDim.x;
+  const auto weight = [&](unsigned long long x) {
+    return set.weight(value_of_key<T>(static_cast<uint32_t>(x)));
+  };
+  const unsigned long long* list = cta_sort(sh->list, n);
   const int per = (n + nt - 1) / nt;
   const int a = min(n, tid * per), b = min(n, a + per);
   unsigned long long own = 0, all;
-  for (int i = a; i < b; ++i) own += weight(candidate_key(list[i]));
-  unsigned long long run = cta_scan(c, own, all);
-  if (k > 0) whole = all;
-  // How many of the front are kept: their running weight is below the target
-  // before them.
-  unsigned long long target = ~0ull;
-  if (share < 1.0f) {
-    target = static_cast<unsigned long long>(
-        ceil(static_cast<double>(share) * static_cast<double>(whole)));
-    if (target < 1) target = 1;
-  }
-  int kept = 0, end = 0;
-  for (int i = a; i < b; ++i) {
-    const unsigned long long w = weight(candidate_key(list[i]));
-    const bool keep = w != 0 && run < target;
-    if (keep) {
-      ++kept;
-      end = i + 1;
-    }
-    // From here on in index order, the key behind it; the others last.
-    list[i] = keep ? (static_cast<unsigned long long>(candidate_index(list[i])) << 32) |
-                         candidate_key(list[i])
-                   : ~0ull;
-    run += w;
-  }
-  n = static_cast<int>(cta_reduce(c, end, MaxOp(), 1));
-  unsigned long long n_kept;
-  cta_scan(c, kept, n_kept);
-  cta_sort_any(list, n);
-  n = static_cast<int>(n_kept);
-  const int per2 = (n + nt - 1) / nt;
-  const int a2 = min(n, tid * per2), b2 = min(n, a2 + per2);
-  own = 0;
-  for (int i = a2; i < b2; ++i) own += weight(static_cast<uint32_t>(list[i]));
-  run = cta_scan(c, own, all);
-  unsigned long long drawn =
-      static_cast<unsigned long long>(static_cast<double>(u) * static_cast<double>(all));
-  if (drawn > all - 1) drawn = all - 1;
+#pragma unroll 1
+  for (int i = a; i < b; ++i) own += weight(list[i]);
+  unsigned long long run = cta_scan(sh, own, all);
+  const unsigned long long drawn = cta_once(sh, [&]() { return DrawnBy{set.u}(all); });
   if (drawn < run || drawn >= run + own) return;
-  for (int i = a2; i < b2; ++i) {
-    const unsigned long long w = weight(static_cast<uint32_t>(list[i]));
+#pragma unroll 1
+  for (int i = a; i < b; ++i) {
+    const unsigned long long w = weight(list[i]);
     run += w;
     if (drawn < run) {
       p.token[r] = static_cast<int32_t>(list[i] >> 32);
-      p.prob[r] = static_cast<float>(static_cast<double>(w) / static_cast<double>(all));
+      p.prob[r] = __fdiv_rn(static_cast<float>(w), static_cast<float>(all));
       return;
     }
   }
 }
 
-// Candidates asked for where only the weight limits what is kept.
-constexpr int kNucleusWant = 256;
-
+// In CTA 0, with at most kListMax / 2 candidates listed (a sorted list then leaves
+// that half of the room free): sorts them, keeps, draws.  `whole`: the
+// weight of all tokens that min-p leaves, where top-k is off.
 template <typename T>
-__global__ void __launch_bounds__(kRowMaxThreads)
+__device__ __noinline__ void sample_candidates(RowShared* sh, const SampleParams& p, int r, int n,
+                                               const Setting set, unsigned long long whole) {
+  const int tid = threadIdx.x, nt = blockDim.x;
+  const auto weight = [&](uint32_t key) { return set.weight(value_of_key<T>(key)); };
+  unsigned long long* list = cta_sort(sh->list, n);
+  if (set.k > 0) n = min(n, set.k);
+  if (!(set.share < 1.0f)) {
+    // All of them; those without a weight are never drawn.
+#pragma unroll 1
+    for (int i = tid; i < n; i += nt)
+      sh->list[i] = (static_cast<unsigned long long>(candidate_index(list[i])) << 32) | candidate_key(list[i]);
+    draw_listed<T>(sh, p, r, n, set);
+    return;
+  }
+  const int per = (n + nt - 1) / nt;
+  const int a = min(n, tid * per), b = min(n, a + per);
+  unsigned long long own = 0, all;
+#pragma unroll 1
+  for (int i = a; i < b; ++i) own += weight(candidate_key(list[i]));
+  const unsigned long long before = cta_scan(sh, own, all);
+  unsigned long long run = before;
+  if (set.k > 0) whole = all;
+  // Kept are those before which the running weight is below the target.
+  const unsigned long long target = cta_once(sh, [&]() { return set.target(whole); });
+  int kept = 0;
+#pragma unroll 1
+  for (int i = a; i < b; ++i) {
+    const unsigned long long w = weight(candidate_key(list[i]));
+    kept += w != 0 && run < target;
+    run += w;
+  }
+  // (weights fall along the list; should two of them not, by a rounding of 2^x at
+  // min-p, what is kept is still the number of those that pass)
+  unsigned long long n_kept;
+  int at = static_cast<int>(cta_scan(sh, kept, n_kept));
+  run = before;
+#pragma unroll 1
+  for (int i = a; i < b; ++i) {
+    const unsigned long long x = list[i], w = weight(candidate_key(x));
+    // In index order from here on, the key behind it.
+    if (w != 0 && run < target)
+      sh->list[at++] = (static_cast<unsigned long long>(candidate_index(x)) << 32) | candidate_key(x);
+    run += w;
+  }
+  draw_listed<T>(sh, p, r, static_cast<int>(n_kept), set);
+}
+
+// Candidates asked for where only the weight limits what is kept.
+constexpr int kNucleusWant = 128;
+
+template <typename T, bool kCluster>
+__global__ void __launch_bounds__(kCluster ? 512 : 1024, 1)
     sample_rows_kernel(const __grid_constant__ SampleParams p, int ctas) {
   constexpr int kVec = Row<T>::kVec;
   extern __shared__ __align__(16) unsigned char slice_smem[];
   __shared__ RowShared sh;
-  row_begin();
-  RowCta c{&sh, static_cast<int>(cluster_ctarank()), ctas, 0};
-  const int r = blockIdx.x / ctas;
+  using Cta = RowCta<kCluster>;
+  Cta::begin();
+  Cta c(&sh, ctas);
+  const int r = kCluster ? blockIdx.x / ctas : blockIdx.x;
   const T* row = static_cast<const T*>(p.logits) + static_cast<long long>(r) * p.ld;
-  const Slice<T> s = row_slice(row, p.V, c.rank, ctas, slice_smem);
-  if (threadIdx.x == 0) sh.listed = 0;
+  const Slice<T, kCluster> s = row_slice<T, kCluster>(row, p.V, c.rank(), c.ctas(), slice_smem, sh.edge);
+  if (threadIdx.x == 0) sh.listed = sh.noted = 0;
+  const float inf = __uint_as_float(0x7f800000u);
   const float t = p.temperature ? p.temperature[r] : 1.0f;
   const bool greedy = !(t > 0.0f);
-  const float scale = greedy ? kRowLog2e : fminf(fmaxf(__fdiv_rn(kRowLog2e, t), 1e-38f), 3e38f);
-  const float pmin = p.min_p ? fminf(p.min_p[r], 1.0f) : 0.0f;
-  int k = p.top_k ? p.top_k[r] : 0;
-  if (k >= p.V || k < 0) k = 0;
-  const float share = p.top_p ? p.top_p[r] : 1.0f;
-  const float u = p.u[r] > 0.0f ? fminf(p.u[r], 1.0f) : 0.0f;  // NaN: 0
+  Setting set;
+  set.scale = greedy ? kRowLog2e : fminf(fmaxf(__fdiv_rn(kRowLog2e, t), 1e-38f), 3e38f);
+  set.pmin = p.min_p ? fminf(p.min_p[r], 1.0f) : 0.0f;
+  set.k = p.top_k ? p.top_k[r] : 0;
+  if (set.k >= p.V || set.k < 0) set.k = 0;
+  set.share = p.top_p ? p.top_p[r] : 1.0f;
+  set.u = p.u[r] > 0.0f ? fminf(p.u[r], 1.0f) : 0.0f;  // NaN: 0
   // Tokens that decide the row, if a list can hold them.
-  const int want = greedy ? 0 : k > 0 ? (k <= kListMax / 2 ? k : 0) : share < 1.0f || pmin > 0.0f ? kNucleusWant : 0;
+  const int want = greedy ? 0
+                   : set.k > 0 ? (set.k <= kListMax / 4 ? set.k : 0)
+                   : set.share < 1.0f || set.pmin > 0.0f ? kNucleusWant : 0;
 
-  const float thread_max = load_row(s, row);
-  row_begun();
+  const float thread_max = load_row(s);
+  c.begun();
   const Floor floor = row_floor<T>(c, thread_max, p.V <= kListMax ? 0 : want);
-  const float zmax = floor.zmax;
-  const float inf = __uint_as_float(0x7f800000u);
+  const float zmax = set.zmax = floor.zmax;
 
   if (!(fabsf(zmax) < inf) || greedy) {
     // The first of the largest logits; a row without a softmax has no probability.
@@ -251,158 +544,128 @@ __global__ void __launch_bounds__(kRowMaxThreads)
     int first = INT_MAX;
     WeightSum sum;
     uint32_t n = 0;
-    for (int v = threadIdx.x; v < s.n_vec; v += blockDim.x, n += kVec) {
+    for_slice<kCluster ? 4 : 8>(s, [&](int v, const uint4& q) {
       float z[kVec];
-      Row<T>::unpack(s.vec[v], z);
+      Row<T>::unpack(q, z);
+      if (!(vec_max(q, -inf, T()) < zmax)) {
 #pragma unroll
-      for (int e = kVec - 1; e >= 0; --e)
-        if (z[e] == zmax && s.index(v, e) >= s.lo && s.index(v, e) < s.hi) first = min(first, s.index(v, e));
+        for (int e = 0; e < kVec; ++e)
+          if (z[e] == zmax && s.holds(s.index(v) + e)) first = min(first, s.index(v) + e);
+      }
 #pragma unroll
       for (int e = 0; e < kVec; e += 2) {
-        const float2 w = row_exp2_pair(z[e], z[e + 1], zmax, scale);
+        const float2 w = row_exp2_pair(z[e], z[e + 1], zmax, set.scale);
         sum.add(w.x, w.y);
       }
-    }
+      n += kVec;
+    });
+    first = __reduce_min_sync(0xffffffffu, first);
     const unsigned long long ix =
-        cta_reduce(c, static_cast<unsigned long long>(first),
-                   [](unsigned long long a, unsigned long long b) { return a < b ? a : b; }, 1);
-    const unsigned long long v[2] = {cta_reduce(c, sum.sum(n), AddOp()), ix};
+        cta_reduce(&sh, first, [](unsigned long long a, unsigned long long b) { return a < b ? a : b; }, 1);
+    const unsigned long long v[2] = {cta_reduce(&sh, sum.sum(n), AddOp()), ix};
     const Parts parts = cluster_exchange(c, v);
-    if (c.rank == 0 && threadIdx.x == 0) {
+    if (c.rank() == 0 && threadIdx.x == 0) {
       unsigned long long best = parts.of(1)[0];
-      for (int q = 1; q < ctas; ++q) best = min(best, parts.of(1)[q]);
+#pragma unroll 1
+      for (int q = 1; q < c.ctas(); ++q) best = min(best, parts.of(1)[q]);
       p.token[r] = best < static_cast<unsigned long long>(p.V) ? static_cast<int>(best) : 0;
-      p.prob[r] = valid ? static_cast<float>(static_cast<double>(kWeightUnit) /
-                                             static_cast<double>(parts.sum(ctas, 0)))
+      p.prob[r] = valid ? __fdiv_rn(kWeightUnit, static_cast<float>(parts.sum(c.ctas(), 0)))
                         : __uint_as_float(0x7fc00000u);
     }
     return;  // no CTA writes into another from here on
   }
 
-  // One pass: the weight of every token that min-p leaves (not needed under
-  // top-k), and the candidates.
-  const bool listing = want > 0 && (p.V <= kListMax || floor.key > 0);
-  const float low = floor.low<T>();
-  WeightSum sum;
-  uint32_t n = 0, pushed = 0;
-  unsigned long long listed_mass = 0;
-  if (k > 0) {
-    if (listing)
-      for (int v = threadIdx.x; v < s.n_vec; v += blockDim.x)
-        if (!(vec_max(s.vec[v], -inf, T()) < low)) {
-          float z[kVec];
-          Row<T>::unpack(s.vec[v], z);
-          pushed += push_vector(c, s, v, z, floor.key);
+  Kept kept{-inf, INT_MAX};
+  const ShareAll share_all(set);
+  unsigned long long mass;
+  int ix;
+  Bracket br{-3e38f, zmax, false, 0};
+  unsigned long long whole = 0;
+  if (want > 0) {
+    // One pass: the weight of every token that min-p leaves (not needed under
+    // top-k), and the candidates.
+    const bool listing = p.V <= kListMax || floor.key > 0;
+    const float low = floor.low<T>();
+    Noted noted(s.n_vec, low);
+    WeightSum sum;
+    uint32_t n = 0, pushed = 0;
+    unsigned long long listed_mass = 0;
+    if (set.k > 0) {
+      if (listing)
+        for_slice<kCluster ? 4 : 8>(s, [&](int v, const uint4& q) {
+          noted.look<T>(v, q);
+        });
+    } else {
+      for_slice<kCluster ? 4 : 8>(s, [&](int v, const uint4& q) {
+        float z[kVec];
+        Row<T>::unpack(q, z);
+#pragma unroll
+        for (int e = 0; e < kVec; e += 2) {
+          float2 w = row_exp2_pair(z[e], z[e + 1], zmax, set.scale);
+          w.x = w.x < set.pmin ? 0.0f : w.x;
+          w.y = w.y < set.pmin ? 0.0f : w.y;
+          sum.add(w.x, w.y);
         }
-  } else {
-    for (int v = threadIdx.x; v < s.n_vec; v += blockDim.x, n += kVec) {
-      float z[kVec];
-      Row<T>::unpack(s.vec[v], z);
-      bool any = false;
-#pragma unroll
-      for (int e = 0; e < kVec; e += 2) {
-        float2 w = row_exp2_pair(z[e], z[e + 1], zmax, scale);
-        w.x = w.x < pmin ? 0.0f : w.x;
-        w.y = w.y < pmin ? 0.0f : w.y;
-        sum.add(w.x, w.y);
-        any |= z[e] >= low || z[e + 1] >= low;
+        n += kVec;
+        if (listing) noted.look<T>(v, q);
+      });
+    }
+    if (listing)
+      pushed = push_noted<T>(c, s, noted, [&](float z) {
+        if (set.k == 0) listed_mass += set.weight(z);
+      });
+    const unsigned long long sums[3] = {sum.sum(n), listed_mass, pushed};
+    const Parts parts = exchange_sums(c, sums);
+    whole = parts.sum(c.ctas(), 0);
+    const unsigned long long target =
+        set.k == 0 && set.share < 1.0f ? cta_once(&sh, [&]() { return set.target(whole); }) : whole;
+    const unsigned long long n_listed = parts.sum(c.ctas(), 2);
+    if (listing && n_listed <= kListMax / 2) {
+      // All that is kept is listed: the first k; or enough weight for the target;
+      // or everything that has a weight.
+      const unsigned long long mass = parts.sum(c.ctas(), 1);
+      if (set.k > 0 || mass >= target) {
+        if (c.rank() == 0) sample_candidates<T>(&sh, p, r, static_cast<int>(n_listed), set, whole);
+        return;
       }
-      if (listing && any) {
-        pushed += push_vector(c, s, v, z, floor.key);
-#pragma unroll
-        for (int e = 0; e < kVec; ++e)
-          if (key_of<T>(z[e]) >= floor.key) {
-            const float w = row_exp2(z[e], zmax, scale);
-            listed_mass += w < pmin ? 0 : weight_of(w);
-          }
+    }
+    if (set.k == 0 && set.share < 1.0f) {
+      // The cut lies below the listed ones or, where they are too many for a list
+      // but heavy enough, among them; and above what could hold no more than the
+      // rest of the weight were every token that light.
+      const unsigned long long light = (whole - target) / p.V;
+      const float e = fmaxf(static_cast<float>(light) - 0.5f, 0.5f) * kOneUnit * 0.99f;
+      br.low = fmaxf(zmax + log2f(fmaxf(e, 0.99f * set.pmin)) / set.scale - 1e-3f * fabsf(zmax), -3e38f);
+      if (listing && low > -inf && n_listed <= kListMax) {  // their weight is known
+        const unsigned long long above = parts.sum(c.ctas(), 1);
+        if (above < target) {
+          br.high = low;
+          br.open = true;
+          br.above = above;
+        } else {
+          br.low = fmaxf(br.low, low);
+        }
       }
     }
   }
-  const unsigned long long sums[3] = {sum.sum(n), listed_mass, pushed};
-  Parts parts = exchange_sums(c, sums);
-  unsigned long long whole = parts.sum(ctas, 0);
-  const unsigned long long n_listed = parts.sum(ctas, 2);
-  if (listing && n_listed <= kListMax) {
-    // All that is kept is listed: the first k; or enough weight for the target;
-    // or min-p's lowest.
-    bool all = k > 0;
-    if (!all && share < 1.0f)
-      all = static_cast<double>(parts.sum(ctas, 1)) >= ceil(static_cast<double>(share) * static_cast<double>(whole));
-    if (!all) all = parts.sum(ctas, 1) == whole;
-    if (all) {
-      if (c.rank == 0)
-        sample_candidates<T>(c, p, r, static_cast<int>(n_listed), k, zmax, scale, pmin, share, u, whole);
-      return;
+  if (set.k > 0) {
+    kept = keep_count<T>(c, s, set.k);
+    if (set.share < 1.0f) {
+      find_index<T>(c, s, ShareKept{share_all, kept}, DrawnNever{}, whole, mass);  // the sum alone
+      br.low = kept.value;
     }
   }
-
-  const uint32_t top = key_of<T>(zmax);
-  Kept kept{0u, INT_MAX};
-  const auto weight = [&](int i, float z) -> unsigned long long {
-    if (!kept.has(key_of<T>(z), i)) return 0;
-    const float e = row_exp2(z, zmax, scale);
-    return e < pmin ? 0 : weight_of(e);
-  };
-  const auto weight_at = [&](int i) { return weight(i, Row<T>::to_float(s.data[i - s.lo])); };
-  const auto weigh = [&]() {
-    unsigned long long m[1] = {0};
-    for_slice(s, [&](int i, float z) { m[0] += weight(i, z); });
-    parts = exchange_sums(c, m);
-    whole = parts.sum(ctas, 0);
-  };
-  // Of the elements that `tie` names, the index of the need-th.
-  const auto nth_tie = [&](uint32_t need, auto&& tie) {
-    unsigned long long m[1] = {0};
-    for (int i = s.lo + threadIdx.x; i < s.hi; i += blockDim.x) m[0] += tie(i);
-    const Parts tied = exchange_sums(c, m);
-    return tell_index(c, find_index(c, s, tied.of(0), need - 1, tie));
-  };
-  if (k > 0) {
-    const Cut cut = find_cut<false>(c, top, k, [&](auto&& f) {
-      for_slice(s, [&](int i, float z) {
-        if (i >= s.lo && i < s.hi) f(key_of<T>(z), 0ull);
-      });
-    });
-    int last = INT_MAX;
-    const uint32_t need = k - cut.above.count;  // of the elements with the cut's key
-    if (need < cut.at.count)
-      last = nth_tie(need, [&](int i) -> unsigned long long {
-        return key_of<T>(Row<T>::to_float(s.data[i - s.lo])) == cut.key;
-      });
-    kept = Kept{cut.key, last};
-    weigh();
-  }
-  if (share < 1.0f) {
-    unsigned long long target = static_cast<unsigned long long>(
-        ceil(static_cast<double>(share) * static_cast<double>(whole)));
-    if (target < 1) target = 1;
-    if (target > whole) target = whole;
-    const Cut cut = find_cut<true>(c, top, target, [&](auto&& f) {
-      for_slice(s, [&](int i, float z) {
-        const unsigned long long w = weight(i, z);
-        if (w) f(key_of<T>(z), w);
-      });
-    });
-    const unsigned long long each = cut.at.mass / cut.at.count;
-    const unsigned long long need = (target - cut.above.mass + each - 1) / each;
-    int last = INT_MAX;
-    if (need < cut.at.count)
-      last = nth_tie(static_cast<uint32_t>(need), [&](int i) -> unsigned long long {
-        return key_of<T>(Row<T>::to_float(s.data[i - s.lo])) == cut.key && weight_at(i) != 0;
-      });
-    if (cut.key == kept.key) last = min(last, kept.last);
-    kept = Kept{cut.key, last};
-    weigh();
-  }
-  unsigned long long drawn =
-      static_cast<unsigned long long>(static_cast<double>(u) * static_cast<double>(whole));
-  if (drawn > whole - 1) drawn = whole - 1;
-  const int ix = find_index(c, s, parts.of(0), drawn, weight_at);
+  if (set.share < 1.0f)
+    kept = keep_weight<T>(c, s, br, cta_once(&sh, [&]() { return set.target(whole); }),
+                          ShareKept{share_all, kept});
+  if (set.k > 0 || set.share < 1.0f)
+    ix = find_index<T>(c, s, ShareKept{share_all, kept}, DrawnBy{set.u}, whole, mass);
+  else
+    ix = find_index<T>(c, s, share_all, DrawnBy{set.u}, whole, mass);
   if (ix >= 0) {
     p.token[r] = ix;
-    p.prob[r] = static_cast<float>(static_cast<double>(weight_at(ix)) / static_cast<double>(whole));
+    p.prob[r] = __fdiv_rn(static_cast<float>(mass), static_cast<float>(whole));
   }
-  row_sync();  // no CTA leaves while a peer may still write into it
 }
 
 struct TopParams {
@@ -423,86 +686,72 @@ struct AddFloatOp {  // on the bits of floats, in a fixed order
   }
 };
 
-template <typename T>
-__global__ void __launch_bounds__(kRowMaxThreads)
+template <typename T, bool kCluster>
+__global__ void __launch_bounds__(kCluster ? 512 : 1024, 1)
     top_rows_kernel(const __grid_constant__ TopParams p, int ctas) {
   constexpr int kVec = Row<T>::kVec;
   extern __shared__ __align__(16) unsigned char slice_smem[];
   __shared__ RowShared sh;
-  row_begin();
-  RowCta c{&sh, static_cast<int>(cluster_ctarank()), ctas, 0};
-  const int r = blockIdx.x / ctas;
+  using Cta = RowCta<kCluster>;
+  Cta::begin();
+  Cta c(&sh, ctas);
+  const int r = kCluster ? blockIdx.x / ctas : blockIdx.x;
   const T* row = static_cast<const T*>(p.logits) + static_cast<long long>(r) * p.ld;
-  const Slice<T> s = row_slice(row, p.V, c.rank, ctas, slice_smem);
-  if (threadIdx.x == 0) sh.listed = 0;
-  const float thread_max = load_row(s, row);
-  row_begun();
+  const Slice<T, kCluster> s = row_slice<T, kCluster>(row, p.V, c.rank(), c.ctas(), slice_smem, sh.edge);
+  if (threadIdx.x == 0) sh.listed = sh.noted = 0;
+  const float inf = __uint_as_float(0x7f800000u);
+  const float thread_max = load_row(s);
+  c.begun();
   const Floor floor = row_floor<T>(c, thread_max, p.V <= kListMax ? 0 : p.K);
   const float zmax = floor.zmax;
   const float scale = __fdiv_rn(kRowLog2e, p.temperature);
   const float low = floor.low<T>();
   // A row of small size is listed whole; a NaN is above every floor.
-  bool listing = p.V <= kListMax || floor.key > 0;
-  float sum = 0.0f;
+  const bool listing = p.V <= kListMax || floor.key > 0;
+  Noted noted(s.n_vec, low);
+  float2 sum2 = make_float2(0.0f, 0.0f);
   uint32_t pushed = 0;
-  for (int v = threadIdx.x; v < s.n_vec; v += blockDim.x) {
+  for_slice<kCluster ? 4 : 8>(s, [&](int v, const uint4& q) {
     float z[kVec];
-    Row<T>::unpack(s.vec[v], z);
-    bool any = false;
+    Row<T>::unpack(q, z);
 #pragma unroll
-    for (int e = 0; e < kVec; ++e) {
-      sum += fast_exp2((z[e] - zmax) * scale);
-      any |= !(z[e] < low);
-    }
-    if (listing && any) pushed += push_vector(c, s, v, z, floor.key);
-  }
-  sum = __uint_as_float(
-      static_cast<uint32_t>(cta_reduce(c, __float_as_uint(sum), AddFloatOp(), 1)));
-  const unsigned long long v[2] = {cta_reduce(c, pushed, AddOp()), __float_as_uint(sum)};
+    for (int e = 0; e < kVec; e += 2)
+      sum2 = __fadd2_rn(sum2, row_exp2_pair(z[e], z[e + 1], zmax, scale));
+        if (listing) noted.look<T>(v, q);
+  });
+  if (listing) pushed = push_noted<T>(c, s, noted, [](float) {});
+  float sum = __uint_as_float(static_cast<uint32_t>(
+      cta_reduce(&sh, __float_as_uint(sum2.x + sum2.y), AddFloatOp(), 1)));
+  const unsigned long long v[2] = {
+      cta_reduce(&sh, pushed, AddOp()), __float_as_uint(sum)};
   const Parts parts = cluster_exchange(c, v);
   sum = __uint_as_float(static_cast<uint32_t>(parts.of(1)[0]));
-  for (int q = 1; q < ctas; ++q) sum += __uint_as_float(static_cast<uint32_t>(parts.of(1)[q]));
-  unsigned long long n = parts.sum(ctas, 0);
-  listing = listing && n <= kListMax;
-  if (!listing) {
-    // Too many equal or too few threads: search for the K-th key, list the K.
-    Kept kept{0u, INT_MAX};
-    const Cut cut = find_cut<false>(c, 0xffffffffu >> (32 - Row<T>::kKeyBits), p.K, [&](auto&& f) {
-      for_slice(s, [&](int i, float z) {
-        if (i >= s.lo && i < s.hi) f(key_of<T>(z), 0ull);
-      });
-    });
-    kept.key = cut.key;
-    const uint32_t need = p.K - cut.above.count;
-    if (need < cut.at.count) {
-      const auto tie = [&](int i) -> unsigned long long {
-        return key_of<T>(Row<T>::to_float(s.data[i - s.lo])) == cut.key;
-      };
-      unsigned long long m[1] = {0};
-      for (int i = s.lo + threadIdx.x; i < s.hi; i += blockDim.x) m[0] += tie(i);
-      const Parts tied = exchange_sums(c, m);
-      kept.last = tell_index(c, find_index(c, s, tied.of(0), need - 1, tie));
-    }
+#pragma unroll 1
+  for (int q = 1; q < c.ctas(); ++q) sum += __uint_as_float(static_cast<uint32_t>(parts.of(1)[q]));
+  uint32_t n = static_cast<uint32_t>(parts.sum(c.ctas(), 0));
+  if (!listing || n > kListMax) {
+    // Too many equal or too few threads: search for the K-th, list the K.
+    const Kept kept = keep_count<T>(c, s, p.K);
     if (threadIdx.x == 0) sh.listed = 0;
-    row_sync();  // nobody reads the bins of the search any more: the list lies over them
-    for_slice(s, [&](int i, float z) {
+    c.sync();
+    const uint32_t cut = key_of<T>(kept.value);
+    for_elements<T>(s, [&](int i, float z) {
       const uint32_t key = key_of<T>(z);
-      if (i >= s.lo && i < s.hi && kept.has(key, i)) push_candidate(c, key, i);
+      if (key > cut || (key == cut && i <= kept.last)) push_candidate(c, key, i);
     });
     n = p.K;
-    row_sync();
+    c.sync();
   }
-  if (c.rank != 0) return;  // nothing is written into the other CTAs any more
-  cta_sort_any(sh.list, static_cast<int>(n));
+  if (c.rank() != 0) return;  // nothing is written into the other CTAs any more
+  const unsigned long long* sorted = cta_sort(sh.list, static_cast<int>(n));
+#pragma unroll 1
   for (int i = threadIdx.x; i < p.K; i += blockDim.x) {
-    const unsigned long long x = sh.list[i];
+    const unsigned long long x = sorted[i];
     p.values[static_cast<long long>(r) * p.K + i] = value_of_key<T>(candidate_key(x));
     p.index[static_cast<long long>(r) * p.K + i] = candidate_index(x);
   }
-  if (threadIdx.x == 0) {
-    const float inf = __uint_as_float(0x7f800000u);
+  if (threadIdx.x == 0)
     p.lse[r] = fabsf(zmax) < inf ? __fdiv_rn(zmax, p.temperature) + logf(sum) : zmax;
-  }
 }
 
 }  // namespace cai
