@@ -12,6 +12,8 @@
 // slice tells the pass over it which elements the record names.
 #pragma once
 
+#include <cstddef>
+
 #include "row_ops.cuh"
 #include "sample.cuh"
 #include "softmax.cuh"
@@ -98,11 +100,13 @@ __host__ __device__ __forceinline__ size_t bitmap_bytes(int slice_elems) {
 
 // Dynamic shared memory: the slice (kCluster), then the bitmap.
 template <typename T, bool kCluster>
-__global__ void __launch_bounds__(kCluster ? 512 : 1024, 1)
+__global__ void __launch_bounds__(512, kCluster ? 1 : 2)
     distill_kernel(const __grid_constant__ DistillParams p, int ctas) {
   constexpr int kVec = Row<T>::kVec;
   extern __shared__ __align__(16) unsigned char slice_smem[];
-  __shared__ RowShared sh;
+  // (without its lists, which come last)
+  __shared__ __align__(16) unsigned char shared_raw[offsetof(RowShared, listed)];
+  RowShared& sh = *reinterpret_cast<RowShared*>(shared_raw);
   __shared__ Record rec;
   using Cta = RowCta<kCluster>;
   Cta::begin();
@@ -111,9 +115,9 @@ __global__ void __launch_bounds__(kCluster ? 512 : 1024, 1)
   const float inf = __uint_as_float(0x7f800000u);
   const T* row = static_cast<const T*>(p.logits) + static_cast<long long>(r) * p.ld;
   T* grow = static_cast<T*>(p.grad) + static_cast<long long>(r) * p.ld_grad;
-  const Slice<T, kCluster> s = row_slice<T, kCluster>(row, p.V, c.rank(), c.ctas(), slice_smem, sh.edge);
+  const Slice<T, kCluster> s = row_slice<T, kCluster>(row, p.V, c.rank(), c.ctas(), slice_smem, kCluster ? 0 : ctas, sh.edge);
   uint32_t* bits = reinterpret_cast<uint32_t*>(
-      slice_smem + (kCluster ? row_slice_bytes(p.V, c.ctas(), sizeof(T)) : 0));
+      slice_smem + (kCluster ? row_slice_bytes(p.V, c.ctas(), sizeof(T)) : static_cast<size_t>(ctas) * 16));
   const bool backward = p.upstream != nullptr;
   const float w = p.weight ? p.weight[r] : 1.0f;
   const uint32_t a_in = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(row + s.lo)) & 15u;
@@ -336,7 +340,7 @@ __global__ void __launch_bounds__(kCluster ? 512 : 1024, 1)
   const float coef = out.s > 0.0f || out.s != out.s ? up * (whole * p_rest - rest) / out.s : 0.0f;
   const auto grad_of = [&](float z) { return coef * fast_exp2(fmaf(z, c2, -ref)); };
   if (a_in == a_out) {
-    for_slice<kCluster ? 4 : 8>(s, [&](int v, const uint4& q) {
+    for_slice<4, true>(s, [&](int v, const uint4& q) {
       float z[kVec];
       Row<T>::unpack(q, z);
 #pragma unroll

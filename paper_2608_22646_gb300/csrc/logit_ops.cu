@@ -31,21 +31,26 @@ struct RowDevice {
   int dev = 0;
   int sms = 0;
   bool ready = false;
+  // Shared memory: what a launch may ask for, and what the kernels have already.
+  size_t limit[3] = {}, fixed[3] = {};
 };
+enum { kSample, kTop, kDistill };
 std::mutex g_row_mutex;
 RowDevice g_row[kMaxDevices];
 
 template <typename K>
-bool open_smem(K* kernel) {
+bool open_smem(K* kernel, int optin, RowDevice* d, int which) {
+  cudaFuncAttributes a{};
+  if (cudaFuncGetAttributes(&a, kernel) != cudaSuccess) return false;
+  const size_t n = static_cast<size_t>(optin) - a.sharedSizeBytes;
+  if (d->limit[which] == 0 || n < d->limit[which]) {
+    d->limit[which] = n;
+    d->fixed[which] = a.sharedSizeBytes;
+  }
   return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                              kRowSliceMax) == cudaSuccess &&
+                              static_cast<int>(n)) == cudaSuccess &&
          cudaFuncSetAttribute(kernel, cudaFuncAttributePreferredSharedMemoryCarveout,
                               cudaSharedmemCarveoutMaxShared) == cudaSuccess;
-}
-
-template <typename K>
-bool open_both(K* cluster, K* alone) {
-  return open_smem(cluster) && open_smem(alone);
 }
 
 // The current device, whose kernels' shared-memory limits are set on first use.
@@ -58,7 +63,7 @@ int row_device(RowDevice** out) {
   RowDevice& d = g_row[dev];
   std::lock_guard<std::mutex> lock(g_row_mutex);
   if (!d.ready) {
-    int major = 0, minor = 0;
+    int major = 0, minor = 0, optin = 0;
     if (cudaDeviceGetAttribute(&major, cudaDevAttrComputeCapabilityMajor, dev) != cudaSuccess ||
         cudaDeviceGetAttribute(&minor, cudaDevAttrComputeCapabilityMinor, dev) != cudaSuccess ||
         cudaDeviceGetAttribute(&d.sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) {
@@ -66,12 +71,20 @@ int row_device(RowDevice** out) {
       return CAI_ERR_CUDA;
     }
     if (major != 10 || minor != 3) return CAI_ERR_UNSUPPORTED;
-    if (!open_both(sample_rows_kernel<float, true>, sample_rows_kernel<float, false>) ||
-        !open_both(sample_rows_kernel<__nv_bfloat16, true>, sample_rows_kernel<__nv_bfloat16, false>) ||
-        !open_both(top_rows_kernel<float, true>, top_rows_kernel<float, false>) ||
-        !open_both(top_rows_kernel<__nv_bfloat16, true>, top_rows_kernel<__nv_bfloat16, false>) ||
-        !open_both(distill_kernel<float, true>, distill_kernel<float, false>) ||
-        !open_both(distill_kernel<__nv_bfloat16, true>, distill_kernel<__nv_bfloat16, false>)) {
+    using bf16 = __nv_bfloat16;
+    if (cudaDeviceGetAttribute(&optin, cudaDevAttrMaxSharedMemoryPerBlockOptin, dev) != cudaSuccess ||
+        !open_smem(sample_rows_kernel<float, true>, optin, &d, kSample) ||
+        !open_smem(sample_rows_kernel<float, false>, optin, &d, kSample) ||
+        !open_smem(sample_rows_kernel<bf16, true>, optin, &d, kSample) ||
+        !open_smem(sample_rows_kernel<bf16, false>, optin, &d, kSample) ||
+        !open_smem(top_rows_kernel<float, true>, optin, &d, kTop) ||
+        !open_smem(top_rows_kernel<float, false>, optin, &d, kTop) ||
+        !open_smem(top_rows_kernel<bf16, true>, optin, &d, kTop) ||
+        !open_smem(top_rows_kernel<bf16, false>, optin, &d, kTop) ||
+        !open_smem(distill_kernel<float, true>, optin, &d, kDistill) ||
+        !open_smem(distill_kernel<float, false>, optin, &d, kDistill) ||
+        !open_smem(distill_kernel<bf16, true>, optin, &d, kDistill) ||
+        !open_smem(distill_kernel<bf16, false>, optin, &d, kDistill)) {
       cudaGetLastError();
       return CAI_ERR_CUDA;
     }
@@ -97,16 +110,16 @@ bool aligned4(const void* p) { return reinterpret_cast<uintptr_t>(p) % 4 == 0; }
 
 // A cluster of CTAs, or one alone, for every row.  `extra`: dynamic shared memory
 // beside the slice, for that many elements of it.
-template <typename P, typename Extra>
+template <typename P>
 int launch_rows(void (*cluster)(P, int), void (*alone)(P, int), const P& p, int M, int V, int elem,
-                int sms, void* stream, Extra&& extra) {
-  const RowPlan plan = row_plan(M, V, elem, sms);
+                const RowDevice& d, int which, void* stream, size_t (*extra)(int)) {
+  const RowPlan plan =
+      row_plan(M, V, elem, d.sms, d.limit[which], d.fixed[which], extra);
   const bool split = plan.ctas > 0;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(static_cast<unsigned>(split ? M * plan.ctas : M));
   cfg.blockDim = dim3(plan.threads);
-  cfg.dynamicSmemBytes = split ? row_slice_bytes(V, plan.ctas, elem) + extra(row_chunk(V, plan.ctas))
-                               : extra(V) + (getenv("ROW_EXTRA") ? atoi(getenv("ROW_EXTRA")) : 0);
+  cfg.dynamicSmemBytes = plan.smem;
   cfg.stream = static_cast<cudaStream_t>(stream);
   cudaLaunchAttribute at[1];
   at[0].id = cudaLaunchAttributeClusterDimension;
@@ -116,7 +129,8 @@ int launch_rows(void (*cluster)(P, int), void (*alone)(P, int), const P& p, int 
   cfg.attrs = at;
   cfg.numAttrs = split ? 1 : 0;
   cudaGetLastError();  // an error left by earlier work is not this call's
-  if (cudaLaunchKernelEx(&cfg, split ? cluster : alone, p, plan.ctas) != cudaSuccess) {
+  if (cudaLaunchKernelEx(&cfg, split ? cluster : alone, p, split ? plan.ctas : plan.room) !=
+      cudaSuccess) {
     cudaGetLastError();
     return CAI_ERR_CUDA;
   }
@@ -142,9 +156,9 @@ extern "C" int cai_sample_rows(const void* logits, int32_t dtype, int64_t ld, in
   SampleParams p{logits, ld, M, V, temperature, top_k, top_p, min_p, u, token, prob};
   return dtype == CAI_BF16
              ? launch_rows(sample_rows_kernel<__nv_bfloat16, true>,
-                           sample_rows_kernel<__nv_bfloat16, false>, p, M, V, 2, d->sms, stream, nothing)
+                           sample_rows_kernel<__nv_bfloat16, false>, p, M, V, 2, *d, kSample, stream, nothing)
              : launch_rows(sample_rows_kernel<float, true>, sample_rows_kernel<float, false>, p, M, V,
-                           4, d->sms, stream, nothing);
+                           4, *d, kSample, stream, nothing);
 }
 
 extern "C" int cai_top_rows(const void* logits, int32_t dtype, int64_t ld, int32_t M, int32_t V,
@@ -164,9 +178,9 @@ extern "C" int cai_top_rows(const void* logits, int32_t dtype, int64_t ld, int32
   TopParams p{logits, ld, M, V, K, static_cast<float>(temperature), values, index, lse};
   return dtype == CAI_BF16
              ? launch_rows(top_rows_kernel<__nv_bfloat16, true>, top_rows_kernel<__nv_bfloat16, false>,
-                           p, M, V, 2, d->sms, stream, nothing)
+                           p, M, V, 2, *d, kTop, stream, nothing)
              : launch_rows(top_rows_kernel<float, true>, top_rows_kernel<float, false>, p, M, V, 4,
-                           d->sms, stream, nothing);
+                           *d, kTop, stream, nothing);
 }
 
 namespace {
@@ -192,9 +206,9 @@ int distill_call(DistillParams& p, int32_t dtype, int64_t ld_grad, void* stream)
   p.ld_grad = ld_grad;
   return dtype == CAI_BF16
              ? launch_rows(distill_kernel<__nv_bfloat16, true>, distill_kernel<__nv_bfloat16, false>, p,
-                           p.M, p.V, 2, d->sms, stream, bitmap_bytes)
+                           p.M, p.V, 2, *d, kDistill, stream, bitmap_bytes)
              : launch_rows(distill_kernel<float, true>, distill_kernel<float, false>, p, p.M, p.V, 4,
-                           d->sms, stream, bitmap_bytes);
+                           *d, kDistill, stream, bitmap_bytes);
 }
 
 }  // namespace

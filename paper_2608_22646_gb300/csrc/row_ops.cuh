@@ -10,7 +10,6 @@
 
 #include <climits>
 #include <cstdint>
-#include <cstdlib>
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 
@@ -19,9 +18,9 @@
 namespace cai {
 
 constexpr int kRowMaxCluster = 8;    // portable cluster size
-constexpr int kRowMaxThreads = 1024;
+constexpr int kRowMaxThreads = 512;
+constexpr int kAloneShare = 2;       // CTAs of 512 threads alone on an SM
 constexpr int kRowMaxWarps = kRowMaxThreads / 32;
-constexpr int kRowSliceMax = 160 * 1024;  // bytes of a row that one CTA keeps
 
 // A vector of 16 bytes of logits as floats.
 template <typename T>
@@ -122,11 +121,21 @@ __device__ __forceinline__ uint4 ld_stream(const uint4* p) {
   return v;
 }
 
+// ... of a row that is read again soon, and for the last time.
+__device__ __forceinline__ uint4 ld_hint(const uint4* p, uint64_t policy) {
+  uint4 v;
+  asm volatile("ld.global.L1::no_allocate.L2::cache_hint.v4.u32 {%0,%1,%2,%3}, [%4], %5;"
+               : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
+               : "l"(p), "l"(policy));
+  return v;
+}
+
 // The slice of a row that this CTA works on: elements [lo, hi).  It is seen as
 // 16-byte vectors of global memory; what the first or last of them holds besides
 // the slice is taken as -inf and never read.  Vector v covers the elements
 // lo - skip + v kVec ...; vectors outside [first, last) are such ends and lie in
-// edge[0] (v = 0) or edge[1].  kKeep: every vector lies in kept[v] once loaded.
+// edge[0] (v = 0) or edge[1].  Once loaded, vector v lies in kept[v] for v < keep;
+// kKeep: every one, the ends too.
 template <typename T, bool kKeep>
 struct Slice {
   static constexpr int kVec = Row<T>::kVec;
@@ -136,10 +145,11 @@ struct Slice {
   uint4* kept;
   uint4* edge;
   int n_vec, first, last;
+  int keep;
   int lo, hi;
   int skip;
 
-  __device__ __forceinline__ Slice(const T* row_, int lo_, int hi_, uint4* kept_, uint4* edge_)
+  __device__ __forceinline__ Slice(const T* row_, int lo_, int hi_, uint4* kept_, int room, uint4* edge_)
       : row(row_), kept(kept_), edge(edge_), lo(lo_), hi(hi_) {
     const uintptr_t at = reinterpret_cast<uintptr_t>(row + lo);
     src = reinterpret_cast<const uint4*>(at & ~static_cast<uintptr_t>(15));
@@ -149,6 +159,7 @@ struct Slice {
     first = skip ? 1 : 0;
     last = max(first, span / kVec);
     if (n_vec == 0) first = last = 0;
+    keep = kKeep ? n_vec : min(room, last);
   }
   __device__ __forceinline__ int index(int v) const { return lo - skip + v * kVec; }
   __device__ __forceinline__ bool holds(int i) const { return i >= lo && i < hi; }
@@ -160,80 +171,100 @@ struct Slice {
   __device__ __forceinline__ float value(int i) const {
     return Row<T>::to_float(kKeep ? reinterpret_cast<const T*>(kept)[i - index(0)] : row[i]);
   }
-  // A vector that is no end, and any, from where the slice lies now.
-  __device__ __forceinline__ uint4 body(int v) const { return kKeep ? kept[v] : ld_stream(src + v); }
+  // Any vector from where the slice lies now.
   __device__ __forceinline__ uint4 get(int v) const {
-    if (kKeep) return kept[v];
+    if (kKeep || (v >= first && v < keep)) return kept[v];
     if (v >= first && v < last) return ld_stream(src + v);
     return edge[v != 0 || first == 0];
   }
 };
 
-// Calls f(v, vector) for the vectors v = from, from + step, ... below `end`, all of
-// them no ends, kFlight loads at a time.  The last round is like the others, with
-// fewer loads: one by one its vectors would wait for memory as often as all the
-// rounds before.
-template <int kFlight, typename S, typename F>
-__device__ __forceinline__ void for_body(const S& s, int from, int end, int step, F&& f) {
+// Calls f(v, vector) for the vectors v = from, from + step, ... below `end`, from
+// memory at `src` (shared or global), kFlight loads at a time.  The last round is
+// like the others, with fewer loads: one by one its vectors would wait for memory
+// as often as all the rounds before.
+template <int kFlight, bool kShared, bool kHint = false, typename F>
+__device__ __forceinline__ void for_vectors(const uint4* src, int from, int end, int step, F&& f,
+                                            uint64_t policy = 0) {
 #pragma unroll 1
   for (int v = from; v < end; v += kFlight * step) {
     uint4 r[kFlight];
 #pragma unroll
     for (int j = 0; j < kFlight; ++j)
-      if (v + j * step < end) r[j] = s.body(v + j * step);
+      if (v + j * step < end) r[j] = kShared ? src[v + j * step] : kHint ? ld_hint(src + v + j * step, policy) : ld_stream(src + v + j * step);
 #pragma unroll
     for (int j = 0; j < kFlight; ++j)
       if (v + j * step < end) f(v + j * step, r[j]);
   }
 }
 
-// Calls f(v, vector) for every vector of the slice, each thread its share.
-template <int kFlight, typename T, bool kKeep, typename F>
-__device__ __forceinline__ void for_slice(const Slice<T, kKeep>& s, F&& f) {
-  const int tid = threadIdx.x, step = static_cast<int>(blockDim.x);
+// ... of a loaded slice, from where they lie; its ends are left out (!kKeep).
+template <int kFlight, bool kLast = false, typename T, bool kKeep, typename F>
+__device__ __forceinline__ void for_body(const Slice<T, kKeep>& s, int from, int end, int step, F&& f) {
   if (kKeep) {
-    for_body<kFlight>(s, tid, s.n_vec, step, f);
+    for_vectors<kFlight, true>(s.kept, from, end, step, f);
     return;
   }
-  for_body<kFlight>(s, s.first + tid, s.last, step, f);
-  const int end = s.end_of(tid);
+  if (from < s.first) from += step;
+  for_vectors<kFlight, true>(s.kept, from, min(end, s.keep), step, f);
+  if (from < s.keep) from += (s.keep - from + step - 1) / step * step;
+  if (kLast)
+    for_vectors<kFlight, false, true>(s.src, from, min(end, s.last), step, f, policy_evict_first());
+  else
+    for_vectors<kFlight, false>(s.src, from, min(end, s.last), step, f);
+}
+
+// Calls f(v, vector) for every vector of the slice, each thread its share.  kLast:
+// nothing reads the row again.
+template <int kFlight, bool kLast = false, typename T, bool kKeep, typename F>
+__device__ __forceinline__ void for_slice(const Slice<T, kKeep>& s, F&& f) {
+  const int tid = threadIdx.x, step = static_cast<int>(blockDim.x);
+  for_body<kFlight, kLast>(s, tid, s.n_vec, step, f);
+  const int end = kKeep ? -1 : s.end_of(tid);
   if (end >= 0) f(end, s.get(end));
 }
 
-// The first pass: as for_slice, from global memory; builds the ends and keeps
-// every vector if kKeep.
+// The first pass over the vectors [a, b) but the ends, from global memory; keeps
+// what there is room for.
+template <int kFlight, typename T, bool kKeep, typename F>
+__device__ __forceinline__ void load_part(const Slice<T, kKeep>& s, int a, int b, F&& f) {
+  const int step = static_cast<int>(blockDim.x);
+  int from = threadIdx.x;
+  a = max(a, s.first);
+  if (from < a) from += (a - from + step - 1) / step * step;
+  const auto see = [&](int v, const uint4& r) {
+    if (kKeep || v < s.keep) s.kept[v] = r;
+    f(v, r);
+  };
+  if (kKeep)
+    for_vectors<kFlight, false>(s.src, from, min(b, s.last), step, see);
+  else
+    for_vectors<kFlight, false, true>(s.src, from, min(b, s.last), step, see, policy_evict_last());
+}
+
+// ... and over the ends, which it builds.
+template <typename T, bool kKeep, typename F>
+__device__ __forceinline__ void load_ends(const Slice<T, kKeep>& s, F&& f) {
+  const int end = s.end_of(threadIdx.x);
+  if (end < 0) return;
+  uint4 r;
+  T* d = reinterpret_cast<T*>(&r);
+#pragma unroll
+  for (int e = 0; e < Row<T>::kVec; ++e) {
+    const int i = s.index(end) + e;
+    d[e] = s.holds(i) ? s.row[i] : Row<T>::neg_inf();
+  }
+  if (kKeep)
+    s.kept[end] = r;
+  else
+    s.edge[end != 0 || s.first == 0] = r;
+  f(end, r);
+}
+
 template <int kFlight, typename T, bool kKeep, typename F>
 __device__ __forceinline__ void load_slice(const Slice<T, kKeep>& s, F&& f) {
-  constexpr int kVec = Row<T>::kVec;
-  const int tid = threadIdx.x, step = static_cast<int>(blockDim.x);
-#pragma unroll 1
-  for (int v = s.first + tid; v < s.last; v += kFlight * step) {
-    uint4 r[kFlight];
-#pragma unroll
-    for (int j = 0; j < kFlight; ++j)
-      if (v + j * step < s.last) r[j] = ld_stream(s.src + v + j * step);
-#pragma unroll
-    for (int j = 0; j < kFlight; ++j)
-      if (v + j * step < s.last) {
-        if (kKeep) s.kept[v + j * step] = r[j];
-        f(v + j * step, r[j]);
-      }
-  }
-  const int end = s.end_of(tid);
-  if (end >= 0) {
-    uint4 r;
-    T* d = reinterpret_cast<T*>(&r);
-#pragma unroll
-    for (int e = 0; e < kVec; ++e) {
-      const int i = s.index(end) + e;
-      d[e] = s.holds(i) ? s.row[i] : Row<T>::neg_inf();
-    }
-    if (kKeep)
-      s.kept[end] = r;
-    else
-      s.edge[end != 0 || s.first == 0] = r;
-    f(end, r);
-  }
+  load_part<kFlight>(s, 0, s.n_vec, f);
+  load_ends(s, f);
 }
 
 // Elements per CTA of a row of V over `ctas`: a multiple of 64.
@@ -247,10 +278,10 @@ __host__ __device__ __forceinline__ size_t row_slice_bytes(int V, int ctas, int 
 
 template <typename T, bool kKeep>
 __device__ __forceinline__ Slice<T, kKeep> row_slice(const T* row, int V, int rank, int ctas,
-                                                     void* smem, uint4* edge) {
+                                                     void* smem, int room, uint4* edge) {
   const int chunk = kKeep ? row_chunk(V, ctas) : V;
   const int lo = min(V, rank * chunk);
-  return Slice<T, kKeep>(row, lo, min(V, lo + chunk), static_cast<uint4*>(smem), edge);
+  return Slice<T, kKeep>(row, lo, min(V, lo + chunk), static_cast<uint4*>(smem), room, edge);
 }
 
 // ------------------------------------------------------ reductions, search --
@@ -657,7 +688,7 @@ __device__ __noinline__ int find_index(C& c, const S s, const Share share, const
       }
       n += kVec;
     };
-    for_body<4>(s, !kKept && v < s.first ? v + step : v, kKept ? end : min(end, s.last), step, add);
+    for_body<4>(s, v, end, step, add);
     // The ends, where they are among this thread's vectors.
 #pragma unroll 1
     for (int k = 0; k < 2; ++k) {
@@ -835,23 +866,37 @@ __device__ __noinline__ unsigned long long* cta_sort(unsigned long long* a, int 
   return a;
 }
 
-// How a call's rows are worked on: ctas 0 stands for the form in which a CTA
-// takes a row alone.
+// How a call's rows are worked on: ctas 0 stands for the form in which a CTA takes a
+// row alone, and keeps `room` vectors of it in shared memory.
 struct RowPlan {
   int ctas, threads;
+  int room;
+  size_t smem;  // dynamic
 };
-__host__ __forceinline__ RowPlan row_plan(int M, int V, int elem, int sms) {
-  static const int fc = getenv("ROW_CTAS") ? atoi(getenv("ROW_CTAS")) : -1;
-  static const int ft = getenv("ROW_THREADS") ? atoi(getenv("ROW_THREADS")) : 0;
+// `extra` bytes beside a slice, `limit` the dynamic shared memory there is for one
+// CTA on an SM beside its fixed_smem.
+__host__ __forceinline__ RowPlan row_plan(int M, int V, int elem, int sms, size_t limit,
+                                          size_t fixed_smem, size_t (*extra)(int)) {
+  // A cluster: as few CTAs as keep a slice within 72 KiB, up to four while the
+  // grid leaves SMs idle and slices stay long; 256 threads, whose reductions and
+  // barriers cost less (one row of 126464 bf16, sampled: 4 CTAs of 256 threads
+  // 15.4 us, of 512 16.5, 8 of 256 16.4, 8 of 512 22).
   constexpr size_t kSliceTarget = 72 * 1024;
   int c = 1;
   while (c < kRowMaxCluster && row_slice_bytes(V, c, elem) > kSliceTarget) c *= 2;
   while (c < 4 && static_cast<long long>(M) * c * 2 <= sms && V / c > 4096) c *= 2;
-  if (c > 1 && M >= sms) c = 0;
-  if (fc >= 0) c = fc;
-  int t = c ? 256 : 512;
-  if (ft) t = ft;
-  return RowPlan{c, t};
+  if (c == 1 || M < sms)
+    return RowPlan{c, 256, 0, row_slice_bytes(V, c, elem) + extra(row_chunk(V, c))};
+  // Alone, two on an SM: what shared memory that leaves, in whole rounds of the
+  // CTA's threads.
+  constexpr size_t kReserved = 1024;  // per CTA, by the system
+  const size_t whole = (limit + fixed_smem + kReserved) / kAloneShare;
+  const size_t taken = kReserved + fixed_smem + extra(V);
+  const size_t round = static_cast<size_t>(kRowMaxThreads) * 16;
+  const size_t row = (static_cast<size_t>(V) * elem + 32) / round * round;
+  size_t keep = (whole > taken ? whole - taken : 0) / round * round;
+  if (keep > row) keep = row;
+  return RowPlan{0, kRowMaxThreads, static_cast<int>(keep / 16), keep + extra(V)};
 }
 
 }  // namespace cai

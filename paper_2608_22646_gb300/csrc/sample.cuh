@@ -53,14 +53,6 @@ struct Kept {
   }
 };
 
-// Loads the slice and returns the thread's largest logit.
-template <typename T, bool kKeep>
-__device__ __forceinline__ float load_row(const Slice<T, kKeep>& s) {
-  float m = __uint_as_float(0xff800000u);
-  load_slice<kKeep ? 4 : 8>(s, [&](int, const uint4& v) { m = vec_max(v, m, T()); });
-  return m;
-}
-
 // The row's largest logit, and a key with at least `want` elements of the row at
 // or above it (0: none is known): every warp finds one for its part of them.
 struct Floor {
@@ -175,15 +167,16 @@ struct Noted {
   unsigned long long bits = 0;
   float low;
   int shift;  // of a vector's number to its bit
-  __device__ __forceinline__ Noted(int n_vec, float l) : low(l) {
+  __device__ __forceinline__ explicit Noted(int n_vec) : low(0.0f) {
     shift = __ffs(blockDim.x) - 1;
 #pragma unroll 1
     while (n_vec >> shift >= 64) ++shift;
   }
   template <typename T>
   __device__ __forceinline__ void look(int v, const uint4& q) {
-    if (!(vec_max(q, __uint_as_float(0xff800000u), T()) < low)) bits |= 1ull << (v >> shift);
+    if (!(vec_max(q, __uint_as_float(0xff800000u), T()) < low)) set(v);
   }
+  __device__ __forceinline__ void set(int v) { bits |= 1ull << (v >> shift); }
 };
 
 // After the pass, pushes the elements that are not below the floor, each thread
@@ -207,7 +200,7 @@ __device__ __forceinline__ uint32_t push_noted(const C& c, const S& s, Noted not
 #pragma unroll 1
       for (int j = 0; j < span; ++j, ++at) {
         // (what an end set stands for one of the thread's other vectors)
-        const int v = (k * span + j) * nt + ((first + tid) & (nt - 1));
+        const int v = (k * span + j) * nt + tid;
         if (at < kListMax) sh->note[at] = v >= first && v < last ? static_cast<uint32_t>(v) : ~0u;
       }
     }
@@ -233,6 +226,54 @@ __device__ __forceinline__ uint32_t push_noted(const C& c, const S& s, Noted not
     }
   }
   return pushed;
+}
+
+// The first pass of a row that is looked through for at least `want` largest
+// elements (0: for the largest alone): f(vector) for every vector; returns the
+// floor.  A CTA alone looks during the pass itself, above a floor from the part of
+// the row that it keeps, and then through that part, above the final one: no second
+// pass over the rest.  looked: whether `noted` is complete.
+template <typename T, bool kCluster, typename C, typename F>
+__device__ __forceinline__ Floor load_row(C& c, const Slice<T, kCluster>& s, int want, bool look,
+                                          Noted& noted, bool& looked, F&& f) {
+  const float inf = __uint_as_float(0x7f800000u);
+  float m = -inf;
+  looked = false;
+  if (!kCluster && look && s.keep > 0) {
+    load_part<4>(s, 0, s.keep, [&](int, const uint4& v) {
+      m = vec_max(v, m, T());
+      f(v);
+    });
+    const int warps = static_cast<int>(blockDim.x >> 5);
+    const uint32_t mine = warp_floor<T>(m, (want + warps - 1) / warps);
+    uint32_t* floors = reinterpret_cast<uint32_t*>(c.sh->wred[1]);
+    if ((threadIdx.x & 31) == 0) floors[threadIdx.x >> 5] = mine;
+    __syncthreads();
+    const uint32_t key = __reduce_min_sync(0xffffffffu, floors[threadIdx.x & (warps - 1)]);
+    noted.low = Floor{0.0f, key}.low<T>();
+    looked = key > 0;
+    load_part<4>(s, s.keep, s.n_vec, [&](int v, const uint4& q) {
+      const float top = vec_max(q, -inf, T());
+      m = max_nan(m, top);
+      if (looked && !(top < noted.low)) noted.set(v);
+      f(q);
+    });
+  } else {
+    load_part<4>(s, 0, s.n_vec, [&](int, const uint4& v) {
+      m = vec_max(v, m, T());
+      f(v);
+    });
+  }
+  load_ends(s, [&](int, const uint4& v) {
+    m = vec_max(v, m, T());
+    f(v);
+  });
+  c.begun();
+  const Floor floor = row_floor<T>(c, m, want);
+  noted.low = floor.low<T>();
+  if (looked)
+    for_body<4>(s, threadIdx.x, s.keep, blockDim.x, [&](int v, const uint4& q) { noted.look<T>(v, q); });
+  return floor;
 }
 
 // Every element of the slice, as f(index, value).
@@ -506,7 +547,7 @@ __device__ __noinline__ void sample_candidates(RowShared* sh, const SampleParams
 constexpr int kNucleusWant = 128;
 
 template <typename T, bool kCluster>
-__global__ void __launch_bounds__(kCluster ? 512 : 1024, 1)
+__global__ void __launch_bounds__(512, kCluster ? 1 : 2)
     sample_rows_kernel(const __grid_constant__ SampleParams p, int ctas) {
   constexpr int kVec = Row<T>::kVec;
   extern __shared__ __align__(16) unsigned char slice_smem[];
@@ -516,7 +557,7 @@ __global__ void __launch_bounds__(kCluster ? 512 : 1024, 1)
   Cta c(&sh, ctas);
   const int r = kCluster ? blockIdx.x / ctas : blockIdx.x;
   const T* row = static_cast<const T*>(p.logits) + static_cast<long long>(r) * p.ld;
-  const Slice<T, kCluster> s = row_slice<T, kCluster>(row, p.V, c.rank(), c.ctas(), slice_smem, sh.edge);
+  const Slice<T, kCluster> s = row_slice<T, kCluster>(row, p.V, c.rank(), c.ctas(), slice_smem, kCluster ? 0 : ctas, sh.edge);
   if (threadIdx.x == 0) sh.listed = sh.noted = 0;
   const float inf = __uint_as_float(0x7f800000u);
   const float t = p.temperature ? p.temperature[r] : 1.0f;
@@ -533,9 +574,11 @@ __global__ void __launch_bounds__(kCluster ? 512 : 1024, 1)
                    : set.k > 0 ? (set.k <= kListMax / 4 ? set.k : 0)
                    : set.share < 1.0f || set.pmin > 0.0f ? kNucleusWant : 0;
 
-  const float thread_max = load_row(s);
-  c.begun();
-  const Floor floor = row_floor<T>(c, thread_max, p.V <= kListMax ? 0 : want);
+  Noted noted(s.n_vec);
+  bool looked;
+  const Floor floor = load_row<T, kCluster>(c, s, p.V <= kListMax ? 0 : want,
+                                            want > 0 && set.k > 0 && p.V > kListMax, noted, looked,
+                                            [](const uint4&) {});
   const float zmax = set.zmax = floor.zmax;
 
   if (!(fabsf(zmax) < inf) || greedy) {
@@ -544,7 +587,7 @@ __global__ void __launch_bounds__(kCluster ? 512 : 1024, 1)
     int first = INT_MAX;
     WeightSum sum;
     uint32_t n = 0;
-    for_slice<kCluster ? 4 : 8>(s, [&](int v, const uint4& q) {
+    for_slice<4>(s, [&](int v, const uint4& q) {
       float z[kVec];
       Row<T>::unpack(q, z);
       if (!(vec_max(q, -inf, T()) < zmax)) {
@@ -585,18 +628,15 @@ __global__ void __launch_bounds__(kCluster ? 512 : 1024, 1)
     // One pass: the weight of every token that min-p leaves (not needed under
     // top-k), and the candidates.
     const bool listing = p.V <= kListMax || floor.key > 0;
-    const float low = floor.low<T>();
-    Noted noted(s.n_vec, low);
+    const float low = noted.low;
     WeightSum sum;
     uint32_t n = 0, pushed = 0;
     unsigned long long listed_mass = 0;
     if (set.k > 0) {
-      if (listing)
-        for_slice<kCluster ? 4 : 8>(s, [&](int v, const uint4& q) {
-          noted.look<T>(v, q);
-        });
+      if (listing && !looked)
+        for_slice<4>(s, [&](int v, const uint4& q) { noted.look<T>(v, q); });
     } else {
-      for_slice<kCluster ? 4 : 8>(s, [&](int v, const uint4& q) {
+      for_slice<4>(s, [&](int v, const uint4& q) {
         float z[kVec];
         Row<T>::unpack(q, z);
 #pragma unroll
@@ -687,7 +727,7 @@ struct AddFloatOp {  // on the bits of floats, in a fixed order
 };
 
 template <typename T, bool kCluster>
-__global__ void __launch_bounds__(kCluster ? 512 : 1024, 1)
+__global__ void __launch_bounds__(512, kCluster ? 1 : 2)
     top_rows_kernel(const __grid_constant__ TopParams p, int ctas) {
   constexpr int kVec = Row<T>::kVec;
   extern __shared__ __align__(16) unsigned char slice_smem[];
@@ -697,28 +737,48 @@ __global__ void __launch_bounds__(kCluster ? 512 : 1024, 1)
   Cta c(&sh, ctas);
   const int r = kCluster ? blockIdx.x / ctas : blockIdx.x;
   const T* row = static_cast<const T*>(p.logits) + static_cast<long long>(r) * p.ld;
-  const Slice<T, kCluster> s = row_slice<T, kCluster>(row, p.V, c.rank(), c.ctas(), slice_smem, sh.edge);
+  const Slice<T, kCluster> s = row_slice<T, kCluster>(row, p.V, c.rank(), c.ctas(), slice_smem, kCluster ? 0 : ctas, sh.edge);
   if (threadIdx.x == 0) sh.listed = sh.noted = 0;
   const float inf = __uint_as_float(0x7f800000u);
-  const float thread_max = load_row(s);
-  c.begun();
-  const Floor floor = row_floor<T>(c, thread_max, p.V <= kListMax ? 0 : p.K);
-  const float zmax = floor.zmax;
   const float scale = __fdiv_rn(kRowLog2e, p.temperature);
-  const float low = floor.low<T>();
-  // A row of small size is listed whole; a NaN is above every floor.
-  const bool listing = p.V <= kListMax || floor.key > 0;
-  Noted noted(s.n_vec, low);
+  // The sum of 2^((z - m) scale).  A CTA alone takes it along in the first pass,
+  // relative to the thread's maximum so far.
   float2 sum2 = make_float2(0.0f, 0.0f);
-  uint32_t pushed = 0;
-  for_slice<kCluster ? 4 : 8>(s, [&](int v, const uint4& q) {
+  float m = -inf;
+  const auto add = [&](const uint4& q, float from) {
     float z[kVec];
     Row<T>::unpack(q, z);
 #pragma unroll
     for (int e = 0; e < kVec; e += 2)
-      sum2 = __fadd2_rn(sum2, row_exp2_pair(z[e], z[e + 1], zmax, scale));
-        if (listing) noted.look<T>(v, q);
-  });
+      sum2 = __fadd2_rn(sum2, row_exp2_pair(z[e], z[e + 1], from, scale));
+  };
+  Noted noted(s.n_vec);
+  bool looked;
+  const Floor floor = load_row<T, kCluster>(
+      c, s, p.V <= kListMax ? 0 : p.K, p.V > kListMax, noted, looked, [&](const uint4& q) {
+        if (kCluster) return;
+        const float top = vec_max(q, -inf, T());
+        if (!(top <= m)) {  // a new maximum, or NaN
+          const float f = m == -inf ? 0.0f : fast_exp2((m - top) * scale);
+          sum2 = make_float2(sum2.x * f, sum2.y * f);
+          m = top;
+        }
+        if (m != -inf) add(q, m);
+      });
+  const float zmax = floor.zmax;
+  // A row of small size is listed whole; a NaN is above every floor.
+  const bool listing = p.V <= kListMax || floor.key > 0;
+  uint32_t pushed = 0;
+  if (kCluster || !looked) {
+    sum2 = make_float2(0.0f, 0.0f);
+    for_slice<4>(s, [&](int v, const uint4& q) {
+      add(q, zmax);
+      if (listing) noted.look<T>(v, q);
+    });
+  } else {
+    const float f = m == -inf ? 0.0f : fast_exp2((m - zmax) * scale);
+    sum2 = make_float2(sum2.x * f, sum2.y * f);
+  }
   if (listing) pushed = push_noted<T>(c, s, noted, [](float) {});
   float sum = __uint_as_float(static_cast<uint32_t>(
       cta_reduce(&sh, __float_as_uint(sum2.x + sum2.y), AddFloatOp(), 1)));
