@@ -494,11 +494,18 @@ def cai_test_static_wait_timeout() -> None:
 
 # ------------------------------------------------ operators on rows of logits --
 
+# Codes of the logits' dtypes seen so far, None for those not taken; and of the
+# dtypes of the other arrays, their names (_DTYPE_NAMES).
+_ROW_CODES: dict = {}
+
+
 def _rows(x, what: str) -> tuple[int, int, int, int, int]:
     """(address, dtype code, row stride, M, V) of a 2-D device tensor of rows
     whose elements are adjacent; rows may be any stride of at least V apart."""
-    full = str(x.dtype)
-    code = CAI_BF16 if full == "torch.bfloat16" else CAI_F32 if full == "torch.float32" else None
+    dt = x.dtype
+    code = _ROW_CODES.get(dt, -1)
+    if code == -1:
+        code = _ROW_CODES[dt] = {"torch.bfloat16": CAI_BF16, "torch.float32": CAI_F32}.get(str(dt))
     if code is None or x.ndim != 2 or not x.is_cuda:
         raise ValueError(f"{what}: expected a 2-D torch.bfloat16 or torch.float32 CUDA tensor "
                          f"(got {x.dtype}, shape {tuple(x.shape)}, on {x.device})")
@@ -516,6 +523,8 @@ def _arr(x, what: str, dtype: str, shape: tuple) -> int | None:
     (None stays None)."""
     if x is None:
         return None
+    if x.shape == shape and _DTYPE_NAMES.get(x.dtype) == dtype and x.is_cuda and x.is_contiguous():
+        return x.data_ptr()
     if tuple(x.shape) != shape or not getattr(x, "is_cuda", False):
         raise ValueError(f"{what}: expected a CUDA tensor of shape {shape}, got "
                          f"{tuple(x.shape)} on {getattr(x, 'device', 'the host')}")

@@ -1,6 +1,7 @@
 // Host side of the 4-bit LM head declared in include/cai.h (cai_mx4_*): the
 // handle with the packed weight and the workspace of the packed rows, argument
 // checks and launches.
+#include <cuda.h>
 #include <cuda_runtime.h>
 
 #include <new>
@@ -18,6 +19,9 @@ struct cai_mx4 {
   size_t smem_limit = 0;       // dynamic shared memory a launch may ask for
   uint8_t* w = nullptr;        // packed weight
   uint8_t* rows = nullptr;     // packed rows of the call in progress
+  int pairs = 0;               // CTA pairs resident at once
+  int pair_stages = 0;
+  Mx4PairMaps maps;
   uint32_t* err = nullptr;     // mapped host memory: bits of waits that gave up
   uint32_t* d_err = nullptr;   // its device address
 };
@@ -60,13 +64,16 @@ int tile_rows(int V, int sms) {
 int pack(const cai_mx4* h, const void* src, int dtype, long long rows, long long rows_pad, int tile,
          uint8_t* dst, void* values, cudaStream_t stream) {
   Mx4PackParams p{src, dst, static_cast<__nv_bfloat16*>(values), rows, rows_pad, h->H, h->KB, tile};
+  // A weight: four items a thread; rows, of which there are few: one, on as many
+  // CTAs as that takes.
   const long long blocks = (rows_pad * 2 * h->KB + 15) / 16;
-  const int grid = static_cast<int>(blocks < h->sms * 16ll ? blocks : h->sms * 16ll);
+  const bool many = blocks > h->sms * 16ll;
+  const int grid = static_cast<int>(many ? h->sms * 8ll : blocks);
   cudaGetLastError();  // an error left by earlier work is not this call's
   if (dtype == CAI_BF16)
-    mx4_pack_kernel<__nv_bfloat16><<<grid, 256, 0, stream>>>(p);
+    (many ? mx4_pack_kernel<__nv_bfloat16, 4> : mx4_pack_kernel<__nv_bfloat16, 1>)<<<grid, 256, 0, stream>>>(p);
   else
-    mx4_pack_kernel<float><<<grid, 256, 0, stream>>>(p);
+    (many ? mx4_pack_kernel<float, 2> : mx4_pack_kernel<float, 1>)<<<grid, 256, 0, stream>>>(p);
   if (cudaGetLastError() != cudaSuccess) return CAI_ERR_CUDA;
   return CAI_OK;
 }
@@ -84,6 +91,73 @@ bool launch_product(const Mx4Params& p, int grid, size_t smem, cudaStream_t stre
   cfg.attrs = at;
   cfg.numAttrs = 1;
   return cudaLaunchKernelEx(&cfg, mx4_logits_kernel<T>, p) == cudaSuccess;
+}
+
+typedef CUresult (*EncodeFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*,
+                             const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
+                             const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
+                             CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+// Packed bytes as rows of 128, copied `box` rows at a time as they lie.
+bool encode_rows(EncodeFn fn, CUtensorMap* m, void* base, size_t bytes, int box) {
+  cuuint64_t dims[2] = {128, bytes / 128};
+  cuuint64_t strides[1] = {128};
+  cuuint32_t boxes[2] = {128, static_cast<cuuint32_t>(box)};
+  cuuint32_t ones[2] = {1, 1};
+  return fn(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, base, dims, strides, boxes, ones,
+            CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// The pair kernel's maps, stages and resident pairs.
+int set_up_pairs(cai_mx4* h, size_t w_bytes, size_t r_bytes) {
+  void* fn = nullptr;
+  cudaDriverEntryPointQueryResult q;
+  if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &fn, 12000, cudaEnableDefault, &q) !=
+          cudaSuccess ||
+      q != cudaDriverEntryPointSuccess)
+    return CAI_ERR_CUDA;
+  const EncodeFn encode = reinterpret_cast<EncodeFn>(fn);
+  if (!encode_rows(encode, &h->maps.rows, h->rows, r_bytes, mx4_stage_bytes(kMx4RowTile) / 128) ||
+      !encode_rows(encode, &h->maps.w, h->w, w_bytes, h->tile / 2) ||
+      !encode_rows(encode, &h->maps.scales, h->w, w_bytes, mx4_scale_bytes(h->tile) / 128))
+    return CAI_ERR_CUDA;
+  h->pair_stages = kMx4MaxStages;
+  while (h->pair_stages > 2 && mx4_pair_smem_bytes(h->pair_stages, h->tile) > h->smem_limit) --h->pair_stages;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(static_cast<unsigned>(h->sms & ~1));
+  cfg.blockDim = dim3(kMx4Threads);
+  cfg.dynamicSmemBytes = mx4_pair_smem_bytes(h->pair_stages, h->tile);
+  cudaLaunchAttribute at[1];
+  at[0].id = cudaLaunchAttributeClusterDimension;
+  at[0].val.clusterDim.x = 2;
+  at[0].val.clusterDim.y = 1;
+  at[0].val.clusterDim.z = 1;
+  cfg.attrs = at;
+  cfg.numAttrs = 1;
+  if (cudaOccupancyMaxActiveClusters(&h->pairs, mx4_logits_pair_kernel<float>, &cfg) != cudaSuccess ||
+      h->pairs < 1)
+    return CAI_ERR_CUDA;
+  return CAI_OK;
+}
+
+template <typename T>
+bool launch_pairs(const cai_mx4* h, const Mx4Params& p, int grid, size_t smem, cudaStream_t stream) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(static_cast<unsigned>(grid));
+  cfg.blockDim = dim3(kMx4Threads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = stream;
+  cudaLaunchAttribute at[2];
+  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at[0].val.programmaticStreamSerializationAllowed = 1;
+  at[1].id = cudaLaunchAttributeClusterDimension;
+  at[1].val.clusterDim.x = 2;
+  at[1].val.clusterDim.y = 1;
+  at[1].val.clusterDim.z = 1;
+  cfg.attrs = at;
+  cfg.numAttrs = 2;
+  return cudaLaunchKernelEx(&cfg, mx4_logits_pair_kernel<T>, h->maps, p) == cudaSuccess;
 }
 
 template <typename K>
@@ -115,14 +189,17 @@ int init(cai_mx4* h, const void* W, int32_t dtype, cudaStream_t stream) {
   if (major != 10 || minor != 3) return CAI_ERR_UNSUPPORTED;
   int r = check_weight(h, W, dtype, nullptr);
   if (r != CAI_OK) return r;
-  if (!open_smem(mx4_logits_kernel<float>, optin, &h->smem_limit) ||
+  if (!open_smem(mx4_logits_pair_kernel<float>, optin, &h->smem_limit) ||
+      !open_smem(mx4_logits_pair_kernel<__nv_bfloat16>, optin, &h->smem_limit) ||
+      !open_smem(mx4_logits_kernel<float>, optin, &h->smem_limit) ||
       !open_smem(mx4_logits_kernel<__nv_bfloat16>, optin, &h->smem_limit))
     return CAI_ERR_CUDA;
   h->KB = (h->H + kMx4K - 1) / kMx4K;
   h->tile = tile_rows(h->V, h->sms);
   h->n_vt = (h->V + h->tile - 1) / h->tile;
   const size_t w_bytes = static_cast<size_t>(h->n_vt) * h->KB * mx4_stage_bytes(h->tile);
-  const size_t n_mt = (h->max_rows + kMx4RowTile - 1) / kMx4RowTile;
+  size_t n_mt = (h->max_rows + kMx4RowTile - 1) / kMx4RowTile;
+  if (n_mt > 1) n_mt = (n_mt + 1) / 2 * 2;  // whole tiles of the pair kernel
   const size_t r_bytes = n_mt * h->KB * mx4_stage_bytes(kMx4RowTile);
   void* p = nullptr;
   if ((r = device_alloc(&p, w_bytes)) != CAI_OK) return r;
@@ -134,6 +211,7 @@ int init(cai_mx4* h, const void* W, int32_t dtype, cudaStream_t stream) {
   *h->err = 0;
   if (cudaHostGetDevicePointer(&p, h->err, 0) != cudaSuccess) return CAI_ERR_CUDA;
   h->d_err = static_cast<uint32_t*>(p);
+  if ((r = set_up_pairs(h, w_bytes, r_bytes)) != CAI_OK) return r;
   // Scales of rows past the last, which the product reads with its whole groups.
   if (cudaMemsetAsync(h->w, 0, w_bytes, stream) != cudaSuccess ||
       cudaMemsetAsync(h->rows, 0, r_bytes, stream) != cudaSuccess)
@@ -214,10 +292,22 @@ extern "C" int cai_mx4_logits(cai_mx4* h, const void* rows, int32_t dtype, int32
   p.KB = h->KB;
   p.tile = h->tile;
   p.n_vt = h->n_vt;
-  p.n_mt = (M + kMx4RowTile - 1) / kMx4RowTile;
-  p.a_rows = M >= kMx4RowTile ? kMx4RowTile : (M + 7) / 8 * 8;
-  p.a_bytes = p.a_rows * 128;
   p.err = h->d_err;
+  if (M > kMx4RowTile) {
+    p.n_mt = (M + 2 * kMx4RowTile - 1) / (2 * kMx4RowTile);
+    p.stages = h->pair_stages;
+    const long long tiles = static_cast<long long>(p.n_vt) * p.n_mt;
+    const int grid = 2 * static_cast<int>(tiles < h->pairs ? tiles : h->pairs);
+    const size_t smem = mx4_pair_smem_bytes(p.stages, p.tile);
+    const bool ok = out_dtype == CAI_BF16 ? launch_pairs<__nv_bfloat16>(h, p, grid, smem, s)
+                                          : launch_pairs<float>(h, p, grid, smem, s);
+    if (ok) return CAI_OK;
+    cudaGetLastError();
+    return CAI_ERR_CUDA;
+  }
+  p.n_mt = 1;
+  p.a_rows = (M + 7) / 8 * 8;
+  p.a_bytes = p.a_rows * 128;
   p.stages = kMx4MaxStages;
   while (p.stages > 2 && mx4_smem_bytes(p.stages, p.a_bytes, p.tile) > h->smem_limit) --p.stages;
   const long long tiles = static_cast<long long>(p.n_vt) * p.n_mt;

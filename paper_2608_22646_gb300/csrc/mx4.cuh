@@ -47,21 +47,29 @@ struct Mx4PackParams {
   int H, KB, tile;
 };
 
-// Eight values of a row as floats.
-__device__ __forceinline__ void mx4_load8(const __nv_bfloat16* p, float (&x)[8]) {
-  const uint4 v = *reinterpret_cast<const uint4*>(p);
-  const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+// Eight values of a row, as they lie in memory and as floats.
+template <typename T>
+struct Mx4Eight {
+  uint4 v[sizeof(T) / 2];
+  __device__ __forceinline__ void load(const T* p) {
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    x[2 * i] = __uint_as_float(w[i] << 16);
-    x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+    for (int i = 0; i < static_cast<int>(sizeof(T) / 2); ++i)
+      asm volatile("ld.global.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];"
+                   : "=r"(v[i].x), "=r"(v[i].y), "=r"(v[i].z), "=r"(v[i].w)
+                   : "l"(reinterpret_cast<const uint4*>(p) + i));
   }
-}
-__device__ __forceinline__ void mx4_load8(const float* p, float (&x)[8]) {
-  const float4 a = *reinterpret_cast<const float4*>(p), b = *reinterpret_cast<const float4*>(p + 4);
-  x[0] = a.x, x[1] = a.y, x[2] = a.z, x[3] = a.w;
-  x[4] = b.x, x[5] = b.y, x[6] = b.z, x[7] = b.w;
-}
+  __device__ __forceinline__ void zero() {
+#pragma unroll
+    for (int i = 0; i < static_cast<int>(sizeof(T) / 2); ++i) v[i] = make_uint4(0u, 0u, 0u, 0u);
+  }
+  __device__ __forceinline__ void floats(float (&x)[8]) const {
+    const uint32_t* w = reinterpret_cast<const uint32_t*>(v);
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      x[i] = sizeof(T) == 4 ? __uint_as_float(w[i])
+                            : __uint_as_float(i & 1 ? w[i / 2] & 0xffff0000u : w[i / 2] << 16);
+  }
+};
 
 // Two values as E2M1 codes, the first in the low half of a byte.
 __device__ __forceinline__ uint32_t mx4_code2(float lo, float hi) {
@@ -84,67 +92,82 @@ __device__ __forceinline__ float2 mx4_value2(uint32_t byte) {
   return __half22float2(*reinterpret_cast<const __half2*>(&h));
 }
 
-// 16 lanes take 128 values of a row, eight each: four lanes a block.
-template <typename T>
+// 16 lanes take 128 values of a row, eight each: four lanes a block.  A group of
+// 128 values is an item; a thread has kFlight of them in flight (126464 x 4096
+// bf16 with values, 344 us by its bytes: one item 583 us, four KFOUR).
+template <typename T, int kFlight>
 __global__ void __launch_bounds__(256) mx4_pack_kernel(const Mx4PackParams p) {
   grid_launch_dependents();
   const int lane = threadIdx.x & 31, sub = lane & 15;
-  const int per_row = 2 * p.KB;  // groups of 128 values
-  const long long n = p.rows_pad * per_row;
-  const long long step = static_cast<long long>(gridDim.x) * (blockDim.x / 16);
+  const uint32_t per_row = 2 * p.KB;
+  // At most 2^22 rows of 128 items.  Both halves of a warp stay together: there
+  // is an even number of items, and a warp begins at an even one.
+  const uint32_t n = static_cast<uint32_t>(p.rows_pad) * per_row;
+  const uint32_t step = gridDim.x * (blockDim.x / 16);
   const int stage = mx4_stage_bytes(p.tile), groups = (p.tile + 127) / 128;
-  for (long long q = blockIdx.x * (blockDim.x / 16) + (threadIdx.x >> 4) - ((lane >> 4) & 1);; q += step) {
-    // q counts for the warp's first half; both halves stay together.
-    const long long item = q + (lane >> 4);
-    if (q >= n) break;
-    const long long row = item / per_row;
-    const int k128 = static_cast<int>(item - row * per_row);
-    const int k = k128 * 128 + sub * 8;
-    float x[8] = {};
-    if (item < n && row < p.rows && k < p.H) mx4_load8(static_cast<const T*>(p.src) + row * p.H + k, x);
-    float high = 0.0f;
-    bool finite = true;
+#pragma unroll 1
+  for (uint32_t q = blockIdx.x * (blockDim.x / 16) + (threadIdx.x >> 4); (q & ~1u) < n; q += kFlight * step) {
+    Mx4Eight<T> in[kFlight];
+    uint32_t row[kFlight];
+    int k128[kFlight];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      high = fmaxf(high, fabsf(x[i]));
-      finite &= fabsf(x[i]) <= 3.402823466e38f;
+    for (int f = 0; f < kFlight; ++f) {
+      const uint32_t item = q + f * step;
+      row[f] = item / per_row;
+      k128[f] = static_cast<int>(item - row[f] * per_row);
+      const int k = k128[f] * 128 + sub * 8;
+      if (item < n && row[f] < p.rows && k < p.H)
+        in[f].load(static_cast<const T*>(p.src) + static_cast<long long>(row[f]) * p.H + k);
+      else
+        in[f].zero();
     }
-    high = fmaxf(high, __shfl_xor_sync(0xffffffffu, high, 1));
-    high = fmaxf(high, __shfl_xor_sync(0xffffffffu, high, 2));
-    const uint32_t ok = __ballot_sync(0xffffffffu, finite);
-    // The scale's exponent, biased: that of the largest value less 2; 255 (no
-    // number) where a value is none.
-    const int e = static_cast<int>(__float_as_uint(high) >> 23);
-    uint32_t code = e > 2 ? e - 2 : 0;
-    if (((ok >> (lane & 28)) & 15u) != 15u) code = 255;
-    const float inv = __uint_as_float(code == 255 ? 0u : (254u - code) << 23);
-    uint32_t packed = 0;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) packed |= mx4_code2(x[2 * i] * inv, x[2 * i + 1] * inv) << (8 * i);
-    uint32_t scales = 0;
+    for (int f = 0; f < kFlight; ++f) {
+      if (((q + f * step) & ~1u) >= n) break;  // the same in the whole warp
+      float x[8];
+      in[f].floats(x);
+      float high = 0.0f;
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
-      scales |= __shfl_sync(0xffffffffu, code, (lane & 16) + 4 * j) << (8 * j);
-    if (item < n) {
-      const long long t = row / p.tile;
-      const int r = static_cast<int>(row - t * p.tile);
-      uint8_t* base = p.dst + (t * p.KB + (k128 >> 1)) * stage;
-      const int chunk = (k128 & 1) * 4 + (sub >> 2);
+      for (int i = 0; i < 8; ++i) high = fmaxf(high, fabsf(x[i]));
+      bool finite = true;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) finite &= fabsf(x[i]) <= 3.402823466e38f;
+      high = fmaxf(high, __shfl_xor_sync(0xffffffffu, high, 1));
+      high = fmaxf(high, __shfl_xor_sync(0xffffffffu, high, 2));
+      const uint32_t ok = __ballot_sync(0xffffffffu, finite);
+      // The scale's exponent, biased: that of the largest value less 2; 255 (no
+      // number) where a value is none.
+      const int e = static_cast<int>(__float_as_uint(high) >> 23);
+      uint32_t code = e > 2 ? e - 2 : 0;
+      if (((ok >> (lane & 28)) & 15u) != 15u) code = 255;
+      const float inv = __uint_as_float(code == 255 ? 0u : (254u - code) << 23);
+      uint32_t packed = 0;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) packed |= mx4_code2(x[2 * i] * inv, x[2 * i + 1] * inv) << (8 * i);
+      uint32_t scales = 0;
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        scales |= __shfl_sync(0xffffffffu, code, (lane & 16) + 4 * j) << (8 * j);
+      const uint32_t t = row[f] / static_cast<uint32_t>(p.tile);
+      const int r = static_cast<int>(row[f] - t * p.tile), h = k128[f] & 1;
+      uint8_t* base = p.dst + (static_cast<size_t>(t) * p.KB + (k128[f] >> 1)) * stage;
+      const int chunk = h * 4 + (sub >> 2);
       *reinterpret_cast<uint32_t*>(base + r * 128 + ((chunk ^ (r & 7)) << 4) + (sub & 3) * 4) = packed;
       if (sub == 0)
-        *reinterpret_cast<uint32_t*>(base + p.tile * 128 +
-                                     ((k128 & 1) * groups + (r >> 7)) * kMx4ScaleAtom +
+        *reinterpret_cast<uint32_t*>(base + p.tile * 128 + (h * groups + (r >> 7)) * kMx4ScaleAtom +
                                      (r & 31) * 16 + ((r >> 5) & 3) * 4) = scales;
-      if (p.values && row < p.rows && k < p.H) {
+      const int k = k128[f] * 128 + sub * 8;
+      if (p.values && row[f] < p.rows && k < p.H) {
         const float scale = __uint_as_float(code == 255 ? 0x7fc00000u : code ? code << 23 : 0x00400000u);
         uint32_t v[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          const float2 f = mx4_value2((packed >> (8 * i)) & 255u);
-          const __nv_bfloat162 b = __floats2bfloat162_rn(f.x * scale, f.y * scale);
+          const float2 y = mx4_value2((packed >> (8 * i)) & 255u);
+          const __nv_bfloat162 b = __floats2bfloat162_rn(y.x * scale, y.y * scale);
           v[i] = *reinterpret_cast<const uint32_t*>(&b);
         }
-        *reinterpret_cast<uint4*>(p.values + row * p.H + k) = make_uint4(v[0], v[1], v[2], v[3]);
+        __stcs(reinterpret_cast<uint4*>(p.values + static_cast<long long>(row[f]) * p.H + k),
+               make_uint4(v[0], v[1], v[2], v[3]));
       }
     }
   }
@@ -162,22 +185,39 @@ __host__ __device__ constexpr uint32_t idesc_mxf4(uint32_t M, uint32_t N, uint32
 }
 
 // D[tmem] (+)= (A . scales) (B . scales)^T over 64 values, issued by one thread.
+// kPair: over a CTA pair, by the even CTA (see mma_bf16_pair): each CTA has its
+// rows' scales in its tensor memory, and all of W's.
+template <bool kPair>
 __device__ __forceinline__ void mma_mxf4(uint32_t d_tmem, uint64_t adesc, uint64_t bdesc,
                                          uint32_t idesc, uint32_t sfa, uint32_t sfb,
                                          uint32_t accumulate) {
-  asm volatile(
-      "{\n\t.reg .pred p;\n\t"
-      "setp.ne.b32 p, %6, 0;\n\t"
-      "tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n\t}" ::"r"(
-          d_tmem),
-      "l"(adesc), "l"(bdesc), "r"(idesc), "r"(sfa), "r"(sfb), "r"(accumulate)
-      : "memory");
+  if constexpr (kPair)
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %6, 0;\n\t"
+        "tcgen05.mma.cta_group::2.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n\t}" ::"r"(
+            d_tmem),
+        "l"(adesc), "l"(bdesc), "r"(idesc), "r"(sfa), "r"(sfb), "r"(accumulate)
+        : "memory");
+  else
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %6, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n\t}" ::"r"(
+            d_tmem),
+        "l"(adesc), "l"(bdesc), "r"(idesc), "r"(sfa), "r"(sfb), "r"(accumulate)
+        : "memory");
 }
 
 // 32 rows of 16 bytes from shared memory into four columns of all four lane
-// quarters; in order with the MMAs of the same thread.
+// quarters (kPair: in both CTAs, each from its own); in order with the MMAs of the
+// same thread.
+template <bool kPair>
 __device__ __forceinline__ void tmem_cp_scales(uint32_t taddr, uint64_t sdesc) {
-  asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(taddr), "l"(sdesc) : "memory");
+  if constexpr (kPair)
+    asm volatile("tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;" ::"r"(taddr), "l"(sdesc) : "memory");
+  else
+    asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(taddr), "l"(sdesc) : "memory");
 }
 
 // Descriptor of a scale group: no swizzle, 8 rows of 16 bytes 128 bytes apart.
@@ -247,6 +287,80 @@ __device__ __forceinline__ float mx4_out<float>(float x) {
 template <>
 __device__ __forceinline__ __nv_bfloat16 mx4_out<__nv_bfloat16>(float x) {
   return __float2bfloat16_rn(x);
+}
+
+// A warp writes its 32 rows by n_v columns of an accumulator (tensor memory `src`,
+// its lanes) out through shared memory `mine`, so that a row's logits leave as
+// whole 32-byte sectors.  out: the first row's first column; n_rows may be 0 or
+// less.  aligned: out's rows begin at multiples of 16 bytes.
+template <typename T>
+__device__ __forceinline__ void mx4_store_tile(uint32_t src, uint8_t* mine, T* out, long long ld,
+                                               int n_rows, int n_v, bool aligned) {
+  constexpr int kPer16 = 16 / sizeof(T);           // values of a 16-byte store
+  constexpr int kLanes = 32 / kPer16;              // lanes of a row's 32 values
+  const int lane = threadIdx.x & 31;
+  if (n_rows <= 0) return;
+#pragma unroll 1
+  for (int c = 0; c < n_v; c += 32) {
+    uint32_t x[32];
+    tmem_ld_32cols(src + c, x);
+    tmem_ld_wait();
+    uint4* st = reinterpret_cast<uint4*>(mine + lane * kMx4EpiPitch);
+    if constexpr (sizeof(T) == 2) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        uint32_t w[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const __nv_bfloat162 b = __floats2bfloat162_rn(__uint_as_float(x[8 * i + 2 * j]),
+                                                         __uint_as_float(x[8 * i + 2 * j + 1]));
+          w[j] = *reinterpret_cast<const uint32_t*>(&b);
+        }
+        st[i] = make_uint4(w[0], w[1], w[2], w[3]);
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) st[i] = make_uint4(x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]);
+    }
+    __syncwarp();
+    const int left = n_v - c;
+    if (aligned && left >= 32) {
+#pragma unroll
+      for (int i = 0; i < kLanes; ++i) {
+        const int rr = i * (32 / kLanes) + lane / kLanes, q = lane % kLanes;
+        if (rr < n_rows)
+          __stcs(reinterpret_cast<uint4*>(out + static_cast<long long>(rr) * ld + c + q * kPer16),
+                 reinterpret_cast<const uint4*>(mine + rr * kMx4EpiPitch)[q]);
+      }
+    } else if (lane < left) {
+      T* to = out + c + lane;
+      const int n = min(n_rows, 32);
+#pragma unroll 8
+      for (int rr = 0; rr < n; ++rr, to += ld)
+        *to = reinterpret_cast<const T*>(mine + rr * kMx4EpiPitch)[lane];
+    }
+    __syncwarp();
+  }
+}
+
+// The stage's scales into tensor memory and its four MMAs, issued by one thread.
+// a: the rows' codes, scales after them at a + a_bytes; b: W's codes, bs their
+// scales.  sf: the tensor-memory columns of this stage's scales.
+template <bool kPair>
+__device__ __forceinline__ void mx4_issue(uint32_t d, uint32_t a, uint32_t as, uint32_t b, uint32_t bs,
+                                          uint32_t sf, uint32_t groups, uint32_t id0, uint32_t id1,
+                                          bool first) {
+#pragma unroll
+  for (uint32_t h = 0; h < 2; ++h) {
+    tmem_cp_scales<kPair>(sf + 4 * h, sdesc_scales(as + h * kMx4ScaleAtom));
+    for (uint32_t g = 0; g < groups; ++g)
+      tmem_cp_scales<kPair>(sf + 8 + 8 * h + 4 * g, sdesc_scales(bs + (h * groups + g) * kMx4ScaleAtom));
+  }
+  const uint64_t ad = sdesc_k_sw128(a), bd = sdesc_k_sw128(b);
+#pragma unroll
+  for (uint32_t j = 0; j < 4; ++j)
+    mma_mxf4<kPair>(d, ad + 2 * j, bd + 2 * j, j & 1 ? id1 : id0, sf + 4 * (j >> 1), sf + 8 + 8 * (j >> 1),
+                    first && j == 0 ? 0u : 1u);
 }
 
 // One CTA per SM; each takes tiles of 128 rows by `tile` vocabulary rows, those
@@ -346,17 +460,7 @@ __global__ void __launch_bounds__(kMx4Threads, 1) mx4_logits_kernel(const Mx4Par
           const uint32_t b = as + mx4_scale_bytes(kMx4RowTile);
           const uint32_t bs = b + p.tile * 128;
           const uint32_t sf = tmem + kMx4ScaleCol + (turn & 1u) * kMx4ScaleCols;
-#pragma unroll
-          for (uint32_t h = 0; h < 2; ++h) {
-            tmem_cp_scales(sf + 4 * h, sdesc_scales(as + h * kMx4ScaleAtom));
-            for (uint32_t g = 0; g < groups; ++g)
-              tmem_cp_scales(sf + 8 + 8 * h + 4 * g, sdesc_scales(bs + (h * groups + g) * kMx4ScaleAtom));
-          }
-          const uint64_t ad = sdesc_k_sw128(a), bd = sdesc_k_sw128(b);
-#pragma unroll
-          for (uint32_t j = 0; j < 4; ++j)
-            mma_mxf4(d, ad + 2 * j, bd + 2 * j, j & 1 ? id1 : id0, sf + 4 * (j >> 1),
-                     sf + 8 + 8 * (j >> 1), (kb | j) != 0 ? 1u : 0u);
+          mx4_issue<false>(d, a, as, b, bs, sf, groups, id0, id1, kb == 0);
           mma_commit(&empty[r.slot]);
         }
         __syncwarp();
@@ -377,8 +481,6 @@ __global__ void __launch_bounds__(kMx4Threads, 1) mx4_logits_kernel(const Mx4Par
   } else {
     const int quarter = warp & 3;
     uint8_t* mine = staging + quarter * 32 * kMx4EpiPitch;
-    constexpr int kPer16 = 16 / sizeof(T);           // values of a 16-byte store
-    constexpr int kLanes = 32 / kPer16;              // lanes of a row's 32 values
     const bool aligned = (reinterpret_cast<uintptr_t>(p.out) | static_cast<uintptr_t>(p.ld * sizeof(T))) % 16 == 0;
     Mx4Ring acc;
     for (int t = blockIdx.x; t < tiles; t += gridDim.x) {
@@ -386,52 +488,10 @@ __global__ void __launch_bounds__(kMx4Threads, 1) mx4_logits_kernel(const Mx4Par
       tc_fence_after();
       const int vt = t / p.n_mt, mt = t - vt * p.n_mt;
       const int row0 = mt * kMx4RowTile + quarter * 32;
-      const int n_rows = min(32, p.M - row0);  // of this warp; may be 0 or less
       const int v0 = vt * p.tile;
-      const int n_v = min(p.tile, p.V - v0);
-      if (n_rows > 0) {
-        const uint32_t src = tmem + acc.slot * kMx4MaxTile + (static_cast<uint32_t>(quarter * 32) << 16);
-        T* out = static_cast<T*>(p.out) + static_cast<long long>(row0) * p.ld + v0;
-        for (int c = 0; c < n_v; c += 32) {
-          uint32_t x[32];
-          tmem_ld_32cols(src + c, x);
-          tmem_ld_wait();
-          T* st = reinterpret_cast<T*>(mine + lane * kMx4EpiPitch);
-          if constexpr (sizeof(T) == 2) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              uint32_t w[4];
-#pragma unroll
-              for (int j = 0; j < 4; ++j) {
-                const __nv_bfloat162 b = __floats2bfloat162_rn(__uint_as_float(x[8 * i + 2 * j]),
-                                                               __uint_as_float(x[8 * i + 2 * j + 1]));
-                w[j] = *reinterpret_cast<const uint32_t*>(&b);
-              }
-              reinterpret_cast<uint4*>(st)[i] = make_uint4(w[0], w[1], w[2], w[3]);
-            }
-          } else {
-#pragma unroll
-            for (int i = 0; i < 8; ++i)
-              reinterpret_cast<uint4*>(st)[i] = make_uint4(x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]);
-          }
-          __syncwarp();
-          const int left = n_v - c;
-          if (aligned && left >= 32) {
-#pragma unroll
-            for (int i = 0; i < kLanes; ++i) {
-              const int rr = i * (32 / kLanes) + lane / kLanes, q = lane % kLanes;
-              if (rr < n_rows)
-                *reinterpret_cast<uint4*>(out + static_cast<long long>(rr) * p.ld + c + q * kPer16) =
-                    reinterpret_cast<const uint4*>(mine + rr * kMx4EpiPitch)[q];
-            }
-          } else if (lane < left) {
-            for (int rr = 0; rr < n_rows; ++rr)
-              out[static_cast<long long>(rr) * p.ld + c + lane] =
-                  reinterpret_cast<const T*>(mine + rr * kMx4EpiPitch)[lane];
-          }
-          __syncwarp();
-        }
-      }
+      mx4_store_tile<T>(tmem + acc.slot * kMx4MaxTile + (static_cast<uint32_t>(quarter * 32) << 16), mine,
+                        static_cast<T*>(p.out) + static_cast<long long>(row0) * p.ld + v0, p.ld,
+                        p.M - row0, min(p.tile, p.V - v0), aligned);
       tc_fence_before();
       __syncwarp();
       if (lane == 0) mbar_arrive(&acce[acc.slot]);
@@ -443,6 +503,171 @@ __global__ void __launch_bounds__(kMx4Threads, 1) mx4_logits_kernel(const Mx4Par
   if (warp == 1) {
     tc_fence_after();
     tmem_dealloc(tmem, kMx4TmemCols);
+  }
+}
+
+// More than 128 rows: CTA pairs (cta_group::2) on tiles of 256 rows, each CTA with
+// its 128 rows and half of the tile's W.  One CTA on 128 rows takes 46 KiB into its
+// shared memory for MMAs of 0.22 us, more than an SM's share of L2 gives (2048 x
+// 126464 x 4096: 105 KB/us, 464 us); a pair's CTA takes 32 KiB for as much.
+// The packed weight and rows are seen as rows of 128 bytes for the copies, which
+// complete on the even CTA's barriers.
+struct Mx4PairMaps {
+  CUtensorMap rows, w, scales;  // boxes: a row tile's stage, half a tile's codes, its scales
+};
+
+__host__ __device__ inline int mx4_pair_stage(int tile) {
+  return mx4_stage_bytes(kMx4RowTile) + tile / 2 * 128 + mx4_scale_bytes(tile);
+}
+__host__ inline size_t mx4_pair_smem_bytes(int stages, int tile) {
+  return 1024 + static_cast<size_t>(stages) * mx4_pair_stage(tile) + kMx4EpiWarps * 32 * kMx4EpiPitch;
+}
+
+template <typename T>
+__global__ void __launch_bounds__(kMx4Threads, 1)
+    mx4_logits_pair_kernel(const __grid_constant__ Mx4PairMaps maps, const Mx4Params p) {
+  extern __shared__ uint8_t smem_raw[];
+  __shared__ uint64_t full[kMx4MaxStages], empty[kMx4MaxStages], accf[2], acce[2], drain;
+  __shared__ uint32_t tmem_slot;
+  __shared__ volatile int abort_flag;
+  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) &
+                                             ~static_cast<uintptr_t>(1023));
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t rank = cluster_ctarank();
+  const int pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
+  const int sstage = mx4_pair_stage(p.tile);
+  constexpr int kRowStage = mx4_stage_bytes(kMx4RowTile);
+  uint8_t* staging = smem + static_cast<size_t>(p.stages) * sstage;
+  const int tiles = p.n_vt * p.n_mt;  // of 256 rows
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < p.stages; ++s) {
+      mbar_init(&full[s], 1);
+      mbar_init(&empty[s], 1);
+    }
+    for (int a = 0; a < 2; ++a) {
+      mbar_init(&accf[a], 1);
+      mbar_init(&acce[a], 2 * kMx4EpiWarps);
+    }
+    mbar_init(&drain, 1);
+    abort_flag = 0;
+    fence_mbar_init();
+    prefetch_tmap(&maps.rows);
+    prefetch_tmap(&maps.w);
+    prefetch_tmap(&maps.scales);
+  }
+  if (warp == 1) {
+    tmem_alloc_pair(&tmem_slot, kMx4TmemCols);
+    tmem_relinquish_pair();
+  }
+  tc_fence_before();
+  __syncthreads();
+  cluster_sync();  // barriers of both CTAs initialised, tensor memory allocated
+  tc_fence_after();
+  const uint32_t tmem = tmem_slot;
+  grid_dependency_wait();  // every role, as in the kernel above
+
+  if (warp == 0) {
+    const uint64_t pol = policy_evict_last();
+    const uint32_t full0 = mapa_shared(full, 0);  // the even CTA's barriers
+    const bool leader = elect_one();
+    const int half = p.tile / 2, w_rows = p.tile + mx4_scale_bytes(p.tile) / 128;
+    const uint32_t tx = 2u * static_cast<uint32_t>(sstage);  // of both CTAs
+    Mx4Ring r;
+    int issued = 0;
+    bool ok = true;
+    for (int t = pair; t < tiles && ok; t += pairs) {
+      const int vt = t / p.n_mt, mt = t - vt * p.n_mt;
+      const int w0 = vt * p.KB * w_rows, r0 = (2 * mt + static_cast<int>(rank)) * p.KB * (kRowStage / 128);
+      for (int kb = 0; kb < p.KB; ++kb) {
+        ok = ok && mbar_wait(&empty[r.slot], r.phase ^ 1u, &abort_flag, p.err, kErrWaitEmpty);
+        if (leader && ok) {
+          uint8_t* s = smem + static_cast<size_t>(r.slot) * sstage;
+          const uint32_t bar = full0 + static_cast<uint32_t>(r.slot * 8);
+          // The even CTA arms the stage for both; a copy of the odd one that
+          // completes first leaves the phase open until then.
+          if (rank == 0) mbar_arrive_expect_tx(&full[r.slot], tx);
+          const int w = w0 + kb * w_rows;
+          tma_load_2d_pair(s, &maps.rows, bar, 0, r0 + kb * (kRowStage / 128), pol);
+          tma_load_2d_pair(s + kRowStage, &maps.w, bar, 0, w + static_cast<int>(rank) * half, pol);
+          tma_load_2d_pair(s + kRowStage + half * 128, &maps.scales, bar, 0, w + p.tile, pol);
+        }
+        __syncwarp();
+        issued += ok ? 1 : 0;
+        r.next(p.stages);
+      }
+      ok = __all_sync(0xffffffffu, ok);
+    }
+    if (leader && !ok && rank == 0)
+      for (int i = issued > p.stages ? issued - p.stages : 0; i < issued; ++i)
+        mx4_drain(&full[i % p.stages], static_cast<uint32_t>((i / p.stages) & 1), p.err);
+    __syncwarp();
+  } else if (warp == 1) {
+    if (rank == 0) {
+      const bool leader = elect_one();
+      const uint32_t groups = (p.tile + 127) / 128;
+      const uint32_t id0 = idesc_mxf4(2 * kMx4RowTile, p.tile, 0), id1 = idesc_mxf4(2 * kMx4RowTile, p.tile, 1);
+      Mx4Ring r, acc;
+      uint32_t turn = 0;
+      bool ok = true;
+      for (int t = pair; t < tiles && ok; t += pairs) {
+        ok = __all_sync(0xffffffffu,
+                        mbar_wait_cluster(&acce[acc.slot], acc.phase ^ 1u, &abort_flag, p.err, kErrWaitAccEmpty));
+        if (!ok) break;
+        tc_fence_after();
+        const uint32_t d = tmem + acc.slot * kMx4MaxTile;
+        for (int kb = 0; kb < p.KB; ++kb) {
+          ok = ok && mbar_wait_cluster(&full[r.slot], r.phase, &abort_flag, p.err, kErrWaitFull);
+          tc_fence_after();
+          if (leader && ok) {
+            const uint32_t a = smem_addr(smem) + r.slot * sstage;
+            const uint32_t b = a + kRowStage;
+            mx4_issue<true>(d, a, a + kMx4RowTile * 128, b, b + p.tile / 2 * 128,
+                            tmem + kMx4ScaleCol + (turn & 1u) * kMx4ScaleCols, groups, id0, id1, kb == 0);
+            mma_commit_pair(&empty[r.slot], 0x3);
+          }
+          __syncwarp();
+          ++turn;
+          r.next(p.stages);
+        }
+        ok = __all_sync(0xffffffffu, ok);
+        if (!ok) break;
+        if (leader) mma_commit_pair(&accf[acc.slot], 0x3);
+        __syncwarp();
+        acc.next(2);
+      }
+      if (leader && !ok) {
+        mma_commit_pair(&drain, 0x1);
+        mx4_drain(&drain, 0, p.err);
+      }
+      __syncwarp();
+    }
+  } else {
+    const int quarter = warp & 3;
+    uint8_t* mine = staging + quarter * 32 * kMx4EpiPitch;
+    const uint32_t acce0 = mapa_shared(acce, 0);
+    const bool aligned = (reinterpret_cast<uintptr_t>(p.out) | static_cast<uintptr_t>(p.ld * sizeof(T))) % 16 == 0;
+    Mx4Ring acc;
+    for (int t = pair; t < tiles; t += pairs) {
+      if (!mbar_wait(&accf[acc.slot], acc.phase, &abort_flag, p.err, kErrWaitAccFull)) break;
+      tc_fence_after();
+      const int vt = t / p.n_mt, mt = t - vt * p.n_mt;
+      const int row0 = (2 * mt + static_cast<int>(rank)) * kMx4RowTile + quarter * 32;
+      const int v0 = vt * p.tile;
+      mx4_store_tile<T>(tmem + acc.slot * kMx4MaxTile + (static_cast<uint32_t>(quarter * 32) << 16), mine,
+                        static_cast<T*>(p.out) + static_cast<long long>(row0) * p.ld + v0, p.ld,
+                        p.M - row0, min(p.tile, p.V - v0), aligned);
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive_cluster(acce0 + static_cast<uint32_t>(acc.slot * 8));
+      acc.next(2);
+    }
+  }
+  tc_fence_before();
+  __syncthreads();
+  cluster_sync();  // no CTA leaves while the pair's MMAs or arrivals may touch it
+  if (warp == 1) {
+    tc_fence_after();
+    tmem_dealloc_pair(tmem, kMx4TmemCols);
   }
 }
 
