@@ -20,7 +20,7 @@ struct cai_mx4 {
   uint8_t* w = nullptr;        // packed weight
   uint8_t* rows = nullptr;     // packed rows of the call in progress
   int pairs = 0;               // CTA pairs resident at once
-  int pair_stages = 0;
+  int pair_stages[2] = {};     // by the logits' size: 2 bytes, 4
   Mx4PairMaps maps;
   uint32_t* err = nullptr;     // mapped host memory: bits of waits that gave up
   uint32_t* d_err = nullptr;   // its device address
@@ -122,12 +122,15 @@ int set_up_pairs(cai_mx4* h, size_t w_bytes, size_t r_bytes) {
       !encode_rows(encode, &h->maps.w, h->w, w_bytes, h->tile / 2) ||
       !encode_rows(encode, &h->maps.scales, h->w, w_bytes, mx4_scale_bytes(h->tile) / 128))
     return CAI_ERR_CUDA;
-  h->pair_stages = kMx4MaxStages;
-  while (h->pair_stages > 2 && mx4_pair_smem_bytes(h->pair_stages, h->tile) > h->smem_limit) --h->pair_stages;
+  for (int k = 0; k < 2; ++k) {
+    int n = kMx4MaxStages;
+    while (n > 2 && mx4_pair_smem_bytes(n, h->tile, 2 << k) > h->smem_limit) --n;
+    h->pair_stages[k] = n;
+  }
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(static_cast<unsigned>(h->sms & ~1));
   cfg.blockDim = dim3(kMx4Threads);
-  cfg.dynamicSmemBytes = mx4_pair_smem_bytes(h->pair_stages, h->tile);
+  cfg.dynamicSmemBytes = mx4_pair_smem_bytes(h->pair_stages[1], h->tile, 4);
   cudaLaunchAttribute at[1];
   at[0].id = cudaLaunchAttributeClusterDimension;
   at[0].val.clusterDim.x = 2;
@@ -295,10 +298,10 @@ extern "C" int cai_mx4_logits(cai_mx4* h, const void* rows, int32_t dtype, int32
   p.err = h->d_err;
   if (M > kMx4RowTile) {
     p.n_mt = (M + 2 * kMx4RowTile - 1) / (2 * kMx4RowTile);
-    p.stages = h->pair_stages;
+    p.stages = h->pair_stages[out_dtype == CAI_F32];
     const long long tiles = static_cast<long long>(p.n_vt) * p.n_mt;
     const int grid = 2 * static_cast<int>(tiles < h->pairs ? tiles : h->pairs);
-    const size_t smem = mx4_pair_smem_bytes(p.stages, p.tile);
+    const size_t smem = mx4_pair_smem_bytes(p.stages, p.tile, elem_bytes(out_dtype));
     const bool ok = out_dtype == CAI_BF16 ? launch_pairs<__nv_bfloat16>(h, p, grid, smem, s)
                                           : launch_pairs<float>(h, p, grid, smem, s);
     if (ok) return CAI_OK;
@@ -309,10 +312,10 @@ extern "C" int cai_mx4_logits(cai_mx4* h, const void* rows, int32_t dtype, int32
   p.a_rows = (M + 7) / 8 * 8;
   p.a_bytes = p.a_rows * 128;
   p.stages = kMx4MaxStages;
-  while (p.stages > 2 && mx4_smem_bytes(p.stages, p.a_bytes, p.tile) > h->smem_limit) --p.stages;
+  while (p.stages > 2 && mx4_smem_bytes(p.stages, p.a_bytes, p.tile, elem_bytes(out_dtype)) > h->smem_limit) --p.stages;
   const long long tiles = static_cast<long long>(p.n_vt) * p.n_mt;
   const int grid = static_cast<int>(tiles < h->sms ? tiles : h->sms);
-  const size_t smem = mx4_smem_bytes(p.stages, p.a_bytes, p.tile);
+  const size_t smem = mx4_smem_bytes(p.stages, p.a_bytes, p.tile, elem_bytes(out_dtype));
   const bool ok = out_dtype == CAI_BF16 ? launch_product<__nv_bfloat16>(p, grid, smem, s)
                                         : launch_product<float>(p, grid, smem, s);
   if (!ok) {

@@ -24,7 +24,7 @@ namespace cai {
 
 constexpr int kMx4Block = 32;          // values per scale
 constexpr int kMx4K = 256;             // values of H per stage: 128 bytes of codes
-constexpr int kMx4MaxTile = 224;       // vocabulary rows per tile, at most
+constexpr int kMx4MaxTile = 208;       // vocabulary rows per tile, at most
 constexpr int kMx4RowTile = 128;       // rows of the step per tile (MMA M)
 constexpr int kMx4ScaleAtom = 512;     // scales of 128 rows and 128 values
 
@@ -94,7 +94,7 @@ __device__ __forceinline__ float2 mx4_value2(uint32_t byte) {
 
 // 16 lanes take 128 values of a row, eight each: four lanes a block.  A group of
 // 128 values is an item; a thread has kFlight of them in flight (126464 x 4096
-// bf16 with values, 344 us by its bytes: one item 583 us, four KFOUR).
+// bf16 with values, 344 us by its bytes: one item 485 us, two 490, four 463).
 template <typename T, int kFlight>
 __global__ void __launch_bounds__(256) mx4_pack_kernel(const Mx4PackParams p) {
   grid_launch_dependents();
@@ -226,13 +226,18 @@ __device__ __forceinline__ uint64_t sdesc_scales(uint32_t saddr) {
          (static_cast<uint64_t>(128u >> 4) << 32) | (static_cast<uint64_t>(1u) << 46);
 }
 
-constexpr int kMx4EpiWarps = 4;
+constexpr int kMx4EpiWarps = 8;  // two for each quarter of the rows
 constexpr int kMx4Threads = 64 + 32 * kMx4EpiWarps;
 constexpr uint32_t kMx4TmemCols = 512;
-constexpr uint32_t kMx4ScaleCol = 2 * kMx4MaxTile;  // scales follow the two accumulators
+constexpr uint32_t kMx4AccCol = 224;                // columns between the two accumulators
+constexpr uint32_t kMx4ScaleCol = kMx4AccCol + kMx4MaxTile;  // scales follow them
 constexpr uint32_t kMx4ScaleCols = 24;              // of one stage: 8 of the rows, 16 of W
+constexpr uint32_t kMx4ScaleBufs = 3;
+static_assert(kMx4ScaleCol + kMx4ScaleBufs * kMx4ScaleCols <= kMx4TmemCols, "tensor memory");
 constexpr int kMx4MaxStages = 8;
-constexpr int kMx4EpiPitch = 32 * 4 + 16;           // bytes between staged rows
+
+// Bytes between the rows of 32 values that a warp writes out through shared memory.
+__host__ __device__ constexpr int mx4_pitch(int elem) { return 32 * elem + 16; }
 
 struct Mx4Params {
   const uint8_t* w;      // packed weight
@@ -252,9 +257,9 @@ __host__ __device__ inline int mx4_smem_stage(int a_bytes, int tile) {
 }
 // The MMA reads 128 rows of A whatever was loaded; past the last stage's there
 // is at least that much allocated.
-__host__ inline size_t mx4_smem_bytes(int stages, int a_bytes, int tile) {
+__host__ inline size_t mx4_smem_bytes(int stages, int a_bytes, int tile, int elem) {
   return 1024 + static_cast<size_t>(stages) * mx4_smem_stage(a_bytes, tile) + 16384 +
-         kMx4EpiWarps * 32 * kMx4EpiPitch;
+         kMx4EpiWarps * 32 * mx4_pitch(elem);
 }
 
 struct Mx4Ring {
@@ -292,20 +297,22 @@ __device__ __forceinline__ __nv_bfloat16 mx4_out<__nv_bfloat16>(float x) {
 // A warp writes its 32 rows by n_v columns of an accumulator (tensor memory `src`,
 // its lanes) out through shared memory `mine`, so that a row's logits leave as
 // whole 32-byte sectors.  out: the first row's first column; n_rows may be 0 or
-// less.  aligned: out's rows begin at multiples of 16 bytes.
+// less.  aligned: out's rows begin at multiples of 16 bytes.  part: which of the two
+// warps that share the rows this is; they take 32 columns in turn.
 template <typename T>
 __device__ __forceinline__ void mx4_store_tile(uint32_t src, uint8_t* mine, T* out, long long ld,
-                                               int n_rows, int n_v, bool aligned) {
+                                               int n_rows, int n_v, bool aligned, int part) {
+  constexpr int kPitch = mx4_pitch(sizeof(T));
   constexpr int kPer16 = 16 / sizeof(T);           // values of a 16-byte store
   constexpr int kLanes = 32 / kPer16;              // lanes of a row's 32 values
   const int lane = threadIdx.x & 31;
   if (n_rows <= 0) return;
 #pragma unroll 1
-  for (int c = 0; c < n_v; c += 32) {
+  for (int c = 32 * part; c < n_v; c += 64) {
     uint32_t x[32];
     tmem_ld_32cols(src + c, x);
     tmem_ld_wait();
-    uint4* st = reinterpret_cast<uint4*>(mine + lane * kMx4EpiPitch);
+    uint4* st = reinterpret_cast<uint4*>(mine + lane * kPitch);
     if constexpr (sizeof(T) == 2) {
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
@@ -330,32 +337,33 @@ __device__ __forceinline__ void mx4_store_tile(uint32_t src, uint8_t* mine, T* o
         const int rr = i * (32 / kLanes) + lane / kLanes, q = lane % kLanes;
         if (rr < n_rows)
           __stcs(reinterpret_cast<uint4*>(out + static_cast<long long>(rr) * ld + c + q * kPer16),
-                 reinterpret_cast<const uint4*>(mine + rr * kMx4EpiPitch)[q]);
+                 reinterpret_cast<const uint4*>(mine + rr * kPitch)[q]);
       }
     } else if (lane < left) {
       T* to = out + c + lane;
       const int n = min(n_rows, 32);
 #pragma unroll 8
       for (int rr = 0; rr < n; ++rr, to += ld)
-        *to = reinterpret_cast<const T*>(mine + rr * kMx4EpiPitch)[lane];
+        *to = reinterpret_cast<const T*>(mine + rr * kPitch)[lane];
     }
     __syncwarp();
   }
 }
 
-// The stage's scales into tensor memory and its four MMAs, issued by one thread.
-// a: the rows' codes, scales after them at a + a_bytes; b: W's codes, bs their
-// scales.  sf: the tensor-memory columns of this stage's scales.
+// A stage's scales into tensor memory (columns sf), and its four MMAs, issued by
+// one thread.  as, bs: the scales of the rows and of W; a, b: their codes.
 template <bool kPair>
-__device__ __forceinline__ void mx4_issue(uint32_t d, uint32_t a, uint32_t as, uint32_t b, uint32_t bs,
-                                          uint32_t sf, uint32_t groups, uint32_t id0, uint32_t id1,
-                                          bool first) {
+__device__ __forceinline__ void mx4_issue_scales(uint32_t sf, uint32_t as, uint32_t bs, uint32_t groups) {
 #pragma unroll
   for (uint32_t h = 0; h < 2; ++h) {
     tmem_cp_scales<kPair>(sf + 4 * h, sdesc_scales(as + h * kMx4ScaleAtom));
     for (uint32_t g = 0; g < groups; ++g)
       tmem_cp_scales<kPair>(sf + 8 + 8 * h + 4 * g, sdesc_scales(bs + (h * groups + g) * kMx4ScaleAtom));
   }
+}
+template <bool kPair>
+__device__ __forceinline__ void mx4_issue_mmas(uint32_t d, uint32_t a, uint32_t b, uint32_t sf, uint32_t id0,
+                                               uint32_t id1, bool first) {
   const uint64_t ad = sdesc_k_sw128(a), bd = sdesc_k_sw128(b);
 #pragma unroll
   for (uint32_t j = 0; j < 4; ++j)
@@ -363,10 +371,57 @@ __device__ __forceinline__ void mx4_issue(uint32_t d, uint32_t a, uint32_t as, u
                     first && j == 0 ? 0u : 1u);
 }
 
-// One CTA per SM; each takes tiles of 128 rows by `tile` vocabulary rows, those
-// that share W next to each other in time.  Warp 0 copies stages, warp 1 issues
-// the scales' copies and the MMAs, warps 2-5 write the accumulators out through
-// shared memory, so that a row's logits leave as whole 32-byte sectors.
+// The MMA warp's loop: n_tiles tiles of p.KB stages.  A stage's scales go to one of
+// three places in turn (2048 x 126464 x 4096: one place 451 us, two 416, three 409;
+// copied a stage ahead of their MMAs, 515: the MMAs then wait for the next stage's
+// bytes too).  The six copies of a stage are what keeps a step from its MMAs' time:
+// without them 308 us, without the MMAs 364.
+template <bool kPair>
+__device__ __forceinline__ bool mx4_issue_all(const Mx4Params& p, int n_tiles, uint32_t smem, int sstage,
+                                              uint32_t as_at, uint32_t b_at, uint32_t bs_at, uint32_t tmem,
+                                              uint64_t* full, uint64_t* empty, uint64_t* accf, uint64_t* acce,
+                                              volatile int* abort_flag, bool leader) {
+  constexpr uint32_t kRows = (kPair ? 2 : 1) * kMx4RowTile;
+  const uint32_t groups = (p.tile + 127) / 128;
+  const uint32_t id0 = idesc_mxf4(kRows, p.tile, 0), id1 = idesc_mxf4(kRows, p.tile, 1);
+  const auto wait = [&](uint64_t* bar, uint32_t phase, uint32_t site) {
+    return __all_sync(0xffffffffu, kPair ? mbar_wait_cluster(bar, phase, abort_flag, p.err, site)
+                                         : mbar_wait(bar, phase, abort_flag, p.err, site));
+  };
+  Mx4Ring r, acc;
+  uint32_t buf = 0;
+  for (int t = 0; t < n_tiles; ++t) {
+    if (!wait(&acce[acc.slot], acc.phase ^ 1u, kErrWaitAccEmpty)) return false;
+    tc_fence_after();
+    for (int kb = 0; kb < p.KB; ++kb) {
+      if (!wait(&full[r.slot], r.phase, kErrWaitFull)) return false;
+      tc_fence_after();
+      if (leader) {
+        const uint32_t s = smem + r.slot * sstage;
+        const uint32_t sf = tmem + kMx4ScaleCol + buf * kMx4ScaleCols;
+        mx4_issue_scales<kPair>(sf, s + as_at, s + bs_at, groups);
+        mx4_issue_mmas<kPair>(tmem + acc.slot * kMx4AccCol, s, s + b_at, sf, id0, id1, kb == 0);
+        if (kPair)
+          mma_commit_pair(&empty[r.slot], 0x3);
+        else
+          mma_commit(&empty[r.slot]);
+      }
+      __syncwarp();
+      r.next(p.stages);
+      if (++buf == kMx4ScaleBufs) buf = 0;
+    }
+    if (leader) {
+      if (kPair)
+        mma_commit_pair(&accf[acc.slot], 0x3);
+      else
+        mma_commit(&accf[acc.slot]);
+    }
+    __syncwarp();
+    acc.next(2);
+  }
+  return true;
+}
+
 template <typename T>
 __global__ void __launch_bounds__(kMx4Threads, 1) mx4_logits_kernel(const Mx4Params p) {
   extern __shared__ uint8_t smem_raw[];
@@ -441,46 +496,18 @@ __global__ void __launch_bounds__(kMx4Threads, 1) mx4_logits_kernel(const Mx4Par
     __syncwarp();
   } else if (warp == 1) {
     const bool leader = elect_one();
-    const uint32_t groups = (p.tile + 127) / 128;
-    const uint32_t id0 = idesc_mxf4(kMx4RowTile, p.tile, 0), id1 = idesc_mxf4(kMx4RowTile, p.tile, 1);
-    Mx4Ring r, acc;
-    uint32_t turn = 0;
-    bool ok = true;
-    for (int t = blockIdx.x; t < tiles && ok; t += gridDim.x) {
-      ok = __all_sync(0xffffffffu, mbar_wait(&acce[acc.slot], acc.phase ^ 1u, &abort_flag, p.err, kErrWaitAccEmpty));
-      if (!ok) break;
-      tc_fence_after();
-      const uint32_t d = tmem + acc.slot * kMx4MaxTile;
-      for (int kb = 0; kb < p.KB; ++kb) {
-        ok = ok && mbar_wait(&full[r.slot], r.phase, &abort_flag, p.err, kErrWaitFull);
-        tc_fence_after();
-        if (leader && ok) {
-          const uint32_t a = smem_addr(smem) + r.slot * sstage;
-          const uint32_t as = a + p.a_bytes;
-          const uint32_t b = as + mx4_scale_bytes(kMx4RowTile);
-          const uint32_t bs = b + p.tile * 128;
-          const uint32_t sf = tmem + kMx4ScaleCol + (turn & 1u) * kMx4ScaleCols;
-          mx4_issue<false>(d, a, as, b, bs, sf, groups, id0, id1, kb == 0);
-          mma_commit(&empty[r.slot]);
-        }
-        __syncwarp();
-        ++turn;
-        r.next(p.stages);
-      }
-      ok = __all_sync(0xffffffffu, ok);
-      if (!ok) break;
-      if (leader) mma_commit(&accf[acc.slot]);
-      __syncwarp();
-      acc.next(2);
-    }
+    const int mine = static_cast<int>(blockIdx.x) < tiles ? (tiles - 1 - blockIdx.x) / gridDim.x + 1 : 0;
+    const uint32_t as_at = p.a_bytes, b_at = as_at + mx4_scale_bytes(kMx4RowTile);
+    const bool ok = mx4_issue_all<false>(p, mine, smem_addr(smem), sstage, as_at, b_at, b_at + p.tile * 128, tmem,
+                                         full, empty, accf, acce, &abort_flag, leader);
     if (leader && !ok) {
       mma_commit(&drain);
       mx4_drain(&drain, 0, p.err);
     }
     __syncwarp();
   } else {
-    const int quarter = warp & 3;
-    uint8_t* mine = staging + quarter * 32 * kMx4EpiPitch;
+    const int quarter = warp & 3, part = (warp - 2) >> 2;
+    uint8_t* mine = staging + (warp - 2) * 32 * mx4_pitch(sizeof(T));
     const bool aligned = (reinterpret_cast<uintptr_t>(p.out) | static_cast<uintptr_t>(p.ld * sizeof(T))) % 16 == 0;
     Mx4Ring acc;
     for (int t = blockIdx.x; t < tiles; t += gridDim.x) {
@@ -489,9 +516,9 @@ __global__ void __launch_bounds__(kMx4Threads, 1) mx4_logits_kernel(const Mx4Par
       const int vt = t / p.n_mt, mt = t - vt * p.n_mt;
       const int row0 = mt * kMx4RowTile + quarter * 32;
       const int v0 = vt * p.tile;
-      mx4_store_tile<T>(tmem + acc.slot * kMx4MaxTile + (static_cast<uint32_t>(quarter * 32) << 16), mine,
+      mx4_store_tile<T>(tmem + acc.slot * kMx4AccCol + (static_cast<uint32_t>(quarter * 32) << 16), mine,
                         static_cast<T*>(p.out) + static_cast<long long>(row0) * p.ld + v0, p.ld,
-                        p.M - row0, min(p.tile, p.V - v0), aligned);
+                        p.M - row0, min(p.tile, p.V - v0), aligned, part);
       tc_fence_before();
       __syncwarp();
       if (lane == 0) mbar_arrive(&acce[acc.slot]);
@@ -509,7 +536,7 @@ __global__ void __launch_bounds__(kMx4Threads, 1) mx4_logits_kernel(const Mx4Par
 // More than 128 rows: CTA pairs (cta_group::2) on tiles of 256 rows, each CTA with
 // its 128 rows and half of the tile's W.  One CTA on 128 rows takes 46 KiB into its
 // shared memory for MMAs of 0.22 us, more than an SM's share of L2 gives (2048 x
-// 126464 x 4096: 105 KB/us, 464 us); a pair's CTA takes 32 KiB for as much.
+// 126464 x 4096: 105 KB/us, 459 us); a pair's CTA takes 32 KiB for as much (409).
 // The packed weight and rows are seen as rows of 128 bytes for the copies, which
 // complete on the even CTA's barriers.
 struct Mx4PairMaps {
@@ -519,8 +546,8 @@ struct Mx4PairMaps {
 __host__ __device__ inline int mx4_pair_stage(int tile) {
   return mx4_stage_bytes(kMx4RowTile) + tile / 2 * 128 + mx4_scale_bytes(tile);
 }
-__host__ inline size_t mx4_pair_smem_bytes(int stages, int tile) {
-  return 1024 + static_cast<size_t>(stages) * mx4_pair_stage(tile) + kMx4EpiWarps * 32 * kMx4EpiPitch;
+__host__ inline size_t mx4_pair_smem_bytes(int stages, int tile, int elem) {
+  return 1024 + static_cast<size_t>(stages) * mx4_pair_stage(tile) + kMx4EpiWarps * 32 * mx4_pitch(elem);
 }
 
 template <typename T>
@@ -604,37 +631,10 @@ __global__ void __launch_bounds__(kMx4Threads, 1)
   } else if (warp == 1) {
     if (rank == 0) {
       const bool leader = elect_one();
-      const uint32_t groups = (p.tile + 127) / 128;
-      const uint32_t id0 = idesc_mxf4(2 * kMx4RowTile, p.tile, 0), id1 = idesc_mxf4(2 * kMx4RowTile, p.tile, 1);
-      Mx4Ring r, acc;
-      uint32_t turn = 0;
-      bool ok = true;
-      for (int t = pair; t < tiles && ok; t += pairs) {
-        ok = __all_sync(0xffffffffu,
-                        mbar_wait_cluster(&acce[acc.slot], acc.phase ^ 1u, &abort_flag, p.err, kErrWaitAccEmpty));
-        if (!ok) break;
-        tc_fence_after();
-        const uint32_t d = tmem + acc.slot * kMx4MaxTile;
-        for (int kb = 0; kb < p.KB; ++kb) {
-          ok = ok && mbar_wait_cluster(&full[r.slot], r.phase, &abort_flag, p.err, kErrWaitFull);
-          tc_fence_after();
-          if (leader && ok) {
-            const uint32_t a = smem_addr(smem) + r.slot * sstage;
-            const uint32_t b = a + kRowStage;
-            mx4_issue<true>(d, a, a + kMx4RowTile * 128, b, b + p.tile / 2 * 128,
-                            tmem + kMx4ScaleCol + (turn & 1u) * kMx4ScaleCols, groups, id0, id1, kb == 0);
-            mma_commit_pair(&empty[r.slot], 0x3);
-          }
-          __syncwarp();
-          ++turn;
-          r.next(p.stages);
-        }
-        ok = __all_sync(0xffffffffu, ok);
-        if (!ok) break;
-        if (leader) mma_commit_pair(&accf[acc.slot], 0x3);
-        __syncwarp();
-        acc.next(2);
-      }
+      const int mine = pair < tiles ? (tiles - 1 - pair) / pairs + 1 : 0;
+      const bool ok = mx4_issue_all<true>(p, mine, smem_addr(smem), sstage, kMx4RowTile * 128, kRowStage,
+                                          kRowStage + p.tile / 2 * 128, tmem, full, empty, accf, acce,
+                                          &abort_flag, leader);
       if (leader && !ok) {
         mma_commit_pair(&drain, 0x1);
         mx4_drain(&drain, 0, p.err);
@@ -642,8 +642,8 @@ __global__ void __launch_bounds__(kMx4Threads, 1)
       __syncwarp();
     }
   } else {
-    const int quarter = warp & 3;
-    uint8_t* mine = staging + quarter * 32 * kMx4EpiPitch;
+    const int quarter = warp & 3, part = (warp - 2) >> 2;
+    uint8_t* mine = staging + (warp - 2) * 32 * mx4_pitch(sizeof(T));
     const uint32_t acce0 = mapa_shared(acce, 0);
     const bool aligned = (reinterpret_cast<uintptr_t>(p.out) | static_cast<uintptr_t>(p.ld * sizeof(T))) % 16 == 0;
     Mx4Ring acc;
@@ -653,9 +653,9 @@ __global__ void __launch_bounds__(kMx4Threads, 1)
       const int vt = t / p.n_mt, mt = t - vt * p.n_mt;
       const int row0 = (2 * mt + static_cast<int>(rank)) * kMx4RowTile + quarter * 32;
       const int v0 = vt * p.tile;
-      mx4_store_tile<T>(tmem + acc.slot * kMx4MaxTile + (static_cast<uint32_t>(quarter * 32) << 16), mine,
+      mx4_store_tile<T>(tmem + acc.slot * kMx4AccCol + (static_cast<uint32_t>(quarter * 32) << 16), mine,
                         static_cast<T*>(p.out) + static_cast<long long>(row0) * p.ld + v0, p.ld,
-                        p.M - row0, min(p.tile, p.V - v0), aligned);
+                        p.M - row0, min(p.tile, p.V - v0), aligned, part);
       tc_fence_before();
       __syncwarp();
       if (lane == 0) mbar_arrive_cluster(acce0 + static_cast<uint32_t>(acc.slot * 8));
