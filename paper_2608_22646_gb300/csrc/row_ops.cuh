@@ -624,22 +624,26 @@ __device__ __forceinline__ unsigned long long weight_of(float e) {
          static_cast<long long>(static_cast<int32_t>(__float_as_uint(l) - kMagicBits));
 }
 
-// The sum of up to 511 elements' weights in a thread.
+// The sum of up to 1022 elements' weights in a thread (a row of 2^18 gives 512 and
+// its ends to each of 512 threads).  A weight's high part is at most 2^23, so each
+// element of a pair has a sum of its own.
 struct WeightSum {
-  uint32_t high = 0, low = 0;
+  uint32_t high0 = 0, high1 = 0, low = 0;
   __device__ __forceinline__ void add(float e0, float e1) {
     const float2 e = make_float2(e0, e1), one = make_float2(1.0f, 1.0f);
     const float2 h = __fadd2_rn(e, one);
     const float2 r = __fadd2_rn(e, __fadd2_rn(one, make_float2(-h.x, -h.y)));
     const float2 l = __ffma2_rn(r, make_float2(kWeightUnit, kWeightUnit),
                                 make_float2(12582912.0f, 12582912.0f));
-    high += __float_as_uint(h.x) + __float_as_uint(h.y);
+    high0 += __float_as_uint(h.x);
+    high1 += __float_as_uint(h.y);
     low += __float_as_uint(l.x) + __float_as_uint(l.y);
   }
-  // After n elements.
+  // After n elements, an even number.
   __device__ __forceinline__ unsigned long long sum(uint32_t n) const {
     const long long lo = static_cast<int32_t>(low - n * kMagicBits);
-    return (static_cast<unsigned long long>(high - n * kOneBits) << 17) + lo;
+    const uint32_t ones = n / 2 * kOneBits;
+    return ((static_cast<unsigned long long>(high0 - ones) + (high1 - ones)) << 17) + lo;
   }
 };
 

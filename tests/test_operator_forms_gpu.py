@@ -174,3 +174,23 @@ def test_the_operators_together():
     said = json.loads(out.strip().splitlines()[-1])
     assert said["loss"][1] < 0.8 * said["loss"][0]
     assert 1 <= said["block_steps"] <= 16 and all(0 <= t < 4096 for t in said["tokens"])
+
+
+@pytest.mark.parametrize("M", [2, MANY])
+@pytest.mark.parametrize("V,dtype,offset", [(262144, BF16, 0), (262143, BF16, 5), (262144, F32, 3), (261000, BF16, 0)])
+def test_the_longest_rows_all_alike(M, V, dtype, offset):
+    """Every weight is 1, the most that a sum has to hold: the token is the whole
+    part of u V and its probability 1 / V, both without rounding."""
+    z = rows_of(M, V, dtype, 1, pad=offset, offset=offset)
+    z.fill_(0.25)
+    u = torch.rand(M, generator=torch.Generator().manual_seed(V)).cuda()
+    u[0], u[1] = 0.0, 1.0 - 2.0 ** -24
+    want = np.floor(u.cpu().numpy().astype(np.float64) * V)
+    for kw in ({}, {"min_p": per_row(M, 0.5)}):
+        token, prob = draw(z, u, **kw)
+        assert (token == want).all()
+        assert (prob == np.float32(1) / np.float32(V)).all()
+    token, prob = draw(z, u, temperature=per_row(M, 0.0))
+    assert (token == 0).all() and (prob == np.float32(1) / np.float32(V)).all()
+    half = draw(z, u, top_p=per_row(M, 0.5))[0]
+    assert (half == np.floor(u.cpu().numpy().astype(np.float64) * -(-V // 2))).all()
