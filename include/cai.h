@@ -447,9 +447,9 @@ int cai_test_static_wait_timeout(void);
  * apart, aligned to their element size only.  M >= 0 (0: nothing is launched),
  * 1 <= V <= 262144.  -inf and the type's lowest value mark tokens a row may not
  * take.  Errors of all four: CAI_ERR_ARG (a null, misaligned or host pointer, a
- * bad dtype, ld < V, a temperature that is not above 0 and finite),
- * CAI_ERR_SHAPE (sizes), CAI_ERR_UNSUPPORTED, CAI_ERR_CUDA; nothing is launched
- * then.
+ * bad dtype, ld < V, a temperature T that in 32 bits is not above 0 or not finite,
+ * or log2(e) / T not), CAI_ERR_SHAPE (sizes), CAI_ERR_UNSUPPORTED, CAI_ERR_CUDA;
+ * nothing is launched then.
  */
 #define CAI_BF16 0
 #define CAI_F32 1

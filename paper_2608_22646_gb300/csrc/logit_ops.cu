@@ -106,6 +106,11 @@ int check_rows(const void* p, int32_t dtype, int64_t ld, int32_t M, int32_t V) {
   return CAI_OK;
 }
 
+// Positive, and log2(e) / t a number in 32 bits, as t is.
+bool is_temperature(float t) {
+  return t > 0.0f && std::isfinite(t) && std::isfinite(kRowLog2e / t);
+}
+
 bool aligned4(const void* p) { return reinterpret_cast<uintptr_t>(p) % 4 == 0; }
 
 // A cluster of CTAs, or one alone, for every row.  `extra`: dynamic shared memory
@@ -167,7 +172,8 @@ extern "C" int cai_top_rows(const void* logits, int32_t dtype, int64_t ld, int32
   int r = check_rows(logits, dtype, ld, M, V);
   if (r != CAI_OK) return r;
   if (K < 1 || K > kTopMax || K > V) return CAI_ERR_SHAPE;
-  if (!(temperature > 0.0) || !std::isfinite(temperature)) return CAI_ERR_ARG;
+  const float t = static_cast<float>(temperature);
+  if (!is_temperature(t)) return CAI_ERR_ARG;
   if (M == 0) return CAI_OK;
   if (!values || !index || !lse) return CAI_ERR_ARG;
   RowDevice* d = nullptr;
@@ -175,7 +181,7 @@ extern "C" int cai_top_rows(const void* logits, int32_t dtype, int64_t ld, int32
   const void* ptrs[] = {logits, values, index, lse};
   for (const void* p : ptrs)
     if ((p != logits && !aligned4(p)) || !on_this_device(p, d->dev)) return CAI_ERR_ARG;
-  TopParams p{logits, ld, M, V, K, static_cast<float>(temperature), values, index, lse};
+  TopParams p{logits, ld, M, V, K, t, values, index, lse};
   return dtype == CAI_BF16
              ? launch_rows(top_rows_kernel<__nv_bfloat16, true>, top_rows_kernel<__nv_bfloat16, false>,
                            p, M, V, 2, *d, kTop, stream, nothing)
@@ -190,7 +196,7 @@ int distill_call(DistillParams& p, int32_t dtype, int64_t ld_grad, void* stream)
   if (r != CAI_OK) return r;
   const int e = elem_bytes(dtype);
   if (p.K < 1 || p.K > kTopMax) return CAI_ERR_SHAPE;
-  if (!(p.tau > 0.0f) || !std::isfinite(p.tau)) return CAI_ERR_ARG;
+  if (!is_temperature(p.tau)) return CAI_ERR_ARG;
   if (p.M == 0) return CAI_OK;
   if (!p.top_values || !p.top_index || !p.stats || (!p.loss && (!p.upstream || !p.grad)))
     return CAI_ERR_ARG;

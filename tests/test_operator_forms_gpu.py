@@ -194,3 +194,16 @@ def test_the_longest_rows_all_alike(M, V, dtype, offset):
     assert (token == 0).all() and (prob == np.float32(1) / np.float32(V)).all()
     half = draw(z, u, top_p=per_row(M, 0.5))[0]
     assert (half == np.floor(u.cpu().numpy().astype(np.float64) * -(-V // 2))).all()
+
+
+@pytest.mark.parametrize("temperature", [1e-60, 1e-40, 1e60])
+def test_temperatures_beyond_32_bits_are_refused(temperature):
+    z = rows_of(2, 100, F32, 1)
+    v, i, lse = (torch.empty((2, 4), device="cuda"), torch.empty((2, 4), dtype=torch.int32, device="cuda"),
+                 torch.empty(2, device="cuda"))
+    with pytest.raises(cai.CaiError):
+        cai.cai_top_rows(z, v, i, lse, temperature=temperature)
+    loss, stats = torch.empty(2, device="cuda"), torch.empty((2, 2), device="cuda")
+    v.zero_(), i.zero_()
+    with pytest.raises(cai.CaiError):
+        cai.cai_distill_loss(z, v, i, loss, stats, temperature=temperature)
