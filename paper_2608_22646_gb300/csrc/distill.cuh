@@ -115,7 +115,8 @@ __global__ void __launch_bounds__(512, kCluster ? 1 : 2)
   const float inf = __uint_as_float(0x7f800000u);
   const T* row = static_cast<const T*>(p.logits) + static_cast<long long>(r) * p.ld;
   T* grow = static_cast<T*>(p.grad) + static_cast<long long>(r) * p.ld_grad;
-  const Slice<T, kCluster> s = row_slice<T, kCluster>(row, p.V, c.rank(), c.ctas(), slice_smem, kCluster ? 0 : ctas, sh.edge);
+  const Slice<T, kCluster> s =
+      row_slice<T, kCluster>(row, p.V, c.rank(), c.ctas(), slice_smem, kCluster ? 0 : ctas, sh.edge);
   uint32_t* bits = reinterpret_cast<uint32_t*>(
       slice_smem + (kCluster ? row_slice_bytes(p.V, c.ctas(), sizeof(T)) : static_cast<size_t>(ctas) * 16));
   const bool backward = p.upstream != nullptr;

@@ -51,7 +51,7 @@ int usable(const cai_mx4* h) {
   return *reinterpret_cast<volatile uint32_t*>(h->err) ? CAI_ERR_DEVICE : CAI_OK;
 }
 
-// Vocabulary rows per tile: as few turns over the SMs as tiles of 224 rows
+// Vocabulary rows per tile: as few turns over the SMs as tiles of kMx4MaxTile rows
 // allow, and then tiles as narrow as that many turns allow, so that every SM
 // gets the same share of W.
 int tile_rows(int V, int sms) {
@@ -312,7 +312,8 @@ extern "C" int cai_mx4_logits(cai_mx4* h, const void* rows, int32_t dtype, int32
   p.a_rows = (M + 7) / 8 * 8;
   p.a_bytes = p.a_rows * 128;
   p.stages = kMx4MaxStages;
-  while (p.stages > 2 && mx4_smem_bytes(p.stages, p.a_bytes, p.tile, elem_bytes(out_dtype)) > h->smem_limit) --p.stages;
+  while (p.stages > 2 && mx4_smem_bytes(p.stages, p.a_bytes, p.tile, elem_bytes(out_dtype)) > h->smem_limit)
+    --p.stages;
   const long long tiles = static_cast<long long>(p.n_vt) * p.n_mt;
   const int grid = static_cast<int>(tiles < h->sms ? tiles : h->sms);
   const size_t smem = mx4_smem_bytes(p.stages, p.a_bytes, p.tile, elem_bytes(out_dtype));

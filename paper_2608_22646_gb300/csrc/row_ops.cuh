@@ -191,7 +191,10 @@ __device__ __forceinline__ void for_vectors(const uint4* src, int from, int end,
     uint4 r[kFlight];
 #pragma unroll
     for (int j = 0; j < kFlight; ++j)
-      if (v + j * step < end) r[j] = kShared ? src[v + j * step] : kHint ? ld_hint(src + v + j * step, policy) : ld_stream(src + v + j * step);
+      if (v + j * step < end) {
+        const uint4* p = src + v + j * step;
+        r[j] = kShared ? *p : kHint ? ld_hint(p, policy) : ld_stream(p);
+      }
 #pragma unroll
     for (int j = 0; j < kFlight; ++j)
       if (v + j * step < end) f(v + j * step, r[j]);
@@ -431,17 +434,6 @@ __device__ __forceinline__ Parts cluster_exchange(C& c, const unsigned long long
   return Parts{s};
 }
 
-template <typename C, typename Op>
-__device__ __forceinline__ unsigned long long cluster_reduce(C& c, unsigned long long v,
-                                                             Op op) {
-  const unsigned long long mine[1] = {cta_reduce(c.sh, v, op)};
-  const unsigned long long* s = cluster_exchange(c, mine).of(0);
-  unsigned long long r = s[0];
-#pragma unroll 1
-  for (int i = 1; i < c.ctas(); ++i) r = op(r, s[i]);
-  return r;
-}
-
 struct AddOp {
   __device__ __forceinline__ unsigned long long operator()(unsigned long long a,
                                                            unsigned long long b) const {
@@ -467,19 +459,6 @@ __device__ __forceinline__ Parts exchange_sums(C& c, const unsigned long long (&
   }
   return cluster_exchange(c, r);
 }
-struct MaxOp {
-  __device__ __forceinline__ unsigned long long operator()(unsigned long long a,
-                                                           unsigned long long b) const {
-    return a > b ? a : b;
-  }
-};
-struct MaxNanOp {  // on the bits of a float
-  __device__ __forceinline__ unsigned long long operator()(unsigned long long a,
-                                                           unsigned long long b) const {
-    return __float_as_uint(max_nan(__uint_as_float(static_cast<uint32_t>(a)),
-                                   __uint_as_float(static_cast<uint32_t>(b))));
-  }
-};
 
 __device__ __forceinline__ unsigned long long warp_scan(unsigned long long v) {  // inclusive
 #pragma unroll

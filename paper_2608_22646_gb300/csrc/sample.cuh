@@ -557,7 +557,8 @@ __global__ void __launch_bounds__(512, kCluster ? 1 : 2)
   Cta c(&sh, ctas);
   const int r = kCluster ? blockIdx.x / ctas : blockIdx.x;
   const T* row = static_cast<const T*>(p.logits) + static_cast<long long>(r) * p.ld;
-  const Slice<T, kCluster> s = row_slice<T, kCluster>(row, p.V, c.rank(), c.ctas(), slice_smem, kCluster ? 0 : ctas, sh.edge);
+  const Slice<T, kCluster> s =
+      row_slice<T, kCluster>(row, p.V, c.rank(), c.ctas(), slice_smem, kCluster ? 0 : ctas, sh.edge);
   if (threadIdx.x == 0) sh.listed = sh.noted = 0;
   const float inf = __uint_as_float(0x7f800000u);
   const float t = p.temperature ? p.temperature[r] : 1.0f;
@@ -737,7 +738,8 @@ __global__ void __launch_bounds__(512, kCluster ? 1 : 2)
   Cta c(&sh, ctas);
   const int r = kCluster ? blockIdx.x / ctas : blockIdx.x;
   const T* row = static_cast<const T*>(p.logits) + static_cast<long long>(r) * p.ld;
-  const Slice<T, kCluster> s = row_slice<T, kCluster>(row, p.V, c.rank(), c.ctas(), slice_smem, kCluster ? 0 : ctas, sh.edge);
+  const Slice<T, kCluster> s =
+      row_slice<T, kCluster>(row, p.V, c.rank(), c.ctas(), slice_smem, kCluster ? 0 : ctas, sh.edge);
   if (threadIdx.x == 0) sh.listed = sh.noted = 0;
   const float inf = __uint_as_float(0x7f800000u);
   const float scale = __fdiv_rn(kRowLog2e, p.temperature);
