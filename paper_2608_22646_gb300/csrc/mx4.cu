@@ -64,16 +64,13 @@ int tile_rows(int V, int sms) {
 int pack(const cai_mx4* h, const void* src, int dtype, long long rows, long long rows_pad, int tile,
          uint8_t* dst, void* values, cudaStream_t stream) {
   Mx4PackParams p{src, dst, static_cast<__nv_bfloat16*>(values), rows, rows_pad, h->H, h->KB, tile};
-  // A weight: four items a thread; rows, of which there are few: one, on as many
-  // CTAs as that takes.
-  const long long blocks = (rows_pad * 2 * h->KB + 15) / 16;
-  const bool many = blocks > h->sms * 16ll;
-  const int grid = static_cast<int>(many ? h->sms * 8ll : blocks);
+  const long long blocks = (rows_pad * 2 * h->KB + 31) / 32;
+  const int grid = static_cast<int>(blocks < h->sms * 256ll ? blocks : h->sms * 256ll);
   cudaGetLastError();  // an error left by earlier work is not this call's
   if (dtype == CAI_BF16)
-    (many ? mx4_pack_kernel<__nv_bfloat16, 4> : mx4_pack_kernel<__nv_bfloat16, 1>)<<<grid, 256, 0, stream>>>(p);
+    mx4_pack_kernel<__nv_bfloat16><<<grid, 256, 0, stream>>>(p);
   else
-    (many ? mx4_pack_kernel<float, 2> : mx4_pack_kernel<float, 1>)<<<grid, 256, 0, stream>>>(p);
+    mx4_pack_kernel<float><<<grid, 256, 0, stream>>>(p);
   if (cudaGetLastError() != cudaSuccess) return CAI_ERR_CUDA;
   return CAI_OK;
 }

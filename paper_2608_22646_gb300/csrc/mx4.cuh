@@ -69,6 +69,21 @@ struct Mx4Eight {
       x[i] = sizeof(T) == 4 ? __uint_as_float(w[i])
                             : __uint_as_float(i & 1 ? w[i / 2] & 0xffff0000u : w[i / 2] << 16);
   }
+  // The biased exponent of the largest magnitude, 255 where a value is not finite.
+  // Magnitudes compare as whole numbers, infinities and NaN above all others.
+  __device__ __forceinline__ uint32_t exponent() const {
+    const uint32_t* w = reinterpret_cast<const uint32_t*>(v);
+    if (sizeof(T) == 4) {
+      uint32_t m = w[0] & 0x7fffffffu;
+#pragma unroll
+      for (int i = 1; i < 8; ++i) m = max(m, w[sizeof(T) == 4 ? i : 0] & 0x7fffffffu);
+      return m >> 23;
+    }
+    uint32_t m = w[0] & 0x7fff7fffu;
+#pragma unroll
+    for (int i = 1; i < 4; ++i) m = __vmaxu2(m, w[i] & 0x7fff7fffu);
+    return max(m >> 16, m & 0xffffu) >> 7;
+  }
 };
 
 // Two values as E2M1 codes, the first in the low half of a byte.
@@ -92,84 +107,112 @@ __device__ __forceinline__ float2 mx4_value2(uint32_t byte) {
   return __half22float2(*reinterpret_cast<const __half2*>(&h));
 }
 
-// 16 lanes take 128 values of a row, eight each: four lanes a block.  A group of
-// 128 values is an item; a thread has kFlight of them in flight (126464 x 4096
-// bf16 with values, 344 us by its bytes: one item 485 us, two 490, four 463).
-template <typename T, int kFlight>
+// Where a group of 128 values of a row lies: in the source, and in the packed
+// tiles.  Moves on by a fixed number of groups without a division.
+struct Mx4Place {
+  uint32_t row, k;  // k: which group of the row
+  uint32_t t, r;    // tile, row in it
+  __device__ __forceinline__ Mx4Place(uint32_t item, uint32_t per_row, uint32_t tile) {
+    row = item / per_row;
+    k = item - row * per_row;
+    t = row / tile;
+    r = row - t * tile;
+  }
+  __device__ __forceinline__ void move(const Mx4Place& by, uint32_t per_row, uint32_t tile) {
+    k += by.k;
+    const uint32_t wrap = k >= per_row;
+    k -= wrap ? per_row : 0;
+    row += by.row + wrap;
+    r += by.r + wrap;
+    t += by.t;
+    if (r >= tile) {
+      r -= tile;
+      ++t;
+    }
+  }
+};
+
+// Eight lanes take a group of 128 values: eight values in each half, of which four
+// lanes hold a block.  Bound by its bytes (126464 x 4096 bf16 with values: 373 us,
+// 344 at the copy's rate; without 239, of 195; float32 with values 516, of 497).
+// Sixteen lanes to a group, positions divided out and a separate test for numbers
+// cost 210 instructions for eight values, and 474 us.  Many CTAs of few turns keep
+// more loads in flight than turns of several groups do: 256 CTAs to an SM 373 us,
+// 64 382, 1000 402; with four groups a turn on 8 404, on 32 387.
+template <typename T>
 __global__ void __launch_bounds__(256) mx4_pack_kernel(const Mx4PackParams p) {
   grid_launch_dependents();
-  const int lane = threadIdx.x & 31, sub = lane & 15;
-  const uint32_t per_row = 2 * p.KB;
-  // At most 2^22 rows of 128 items.  Both halves of a warp stay together: there
-  // is an even number of items, and a warp begins at an even one.
+  constexpr uint32_t kItems = 256 / 8;  // of a CTA
+  const int lane = threadIdx.x & 31, sub = lane & 7;
+  const uint32_t per_row = 2 * p.KB, tile = p.tile;
+  // At most 2^22 rows of 128 groups, and some.
   const uint32_t n = static_cast<uint32_t>(p.rows_pad) * per_row;
-  const uint32_t step = gridDim.x * (blockDim.x / 16);
-  const int stage = mx4_stage_bytes(p.tile), groups = (p.tile + 127) / 128;
+  const uint32_t step = gridDim.x * kItems;
+  const uint32_t stage = mx4_stage_bytes(p.tile), groups = (tile + 127) / 128;
+  uint32_t q = blockIdx.x * kItems + (threadIdx.x >> 3);
+  const Mx4Place by(step, per_row, tile);
+  Mx4Place at(q, per_row, tile);
 #pragma unroll 1
-  for (uint32_t q = blockIdx.x * (blockDim.x / 16) + (threadIdx.x >> 4); (q & ~1u) < n; q += kFlight * step) {
-    Mx4Eight<T> in[kFlight];
-    uint32_t row[kFlight];
-    int k128[kFlight];
+  for (; (q & ~3u) < n; q += step) {  // the same in the whole warp
+    const int k = static_cast<int>(at.k) * 128 + sub * 8;
+    const bool there = q < n && at.row < p.rows;
+    const T* src = static_cast<const T*>(p.src) + static_cast<long long>(at.row) * p.H + k;
+    Mx4Eight<T> in[2];
 #pragma unroll
-    for (int f = 0; f < kFlight; ++f) {
-      const uint32_t item = q + f * step;
-      row[f] = item / per_row;
-      k128[f] = static_cast<int>(item - row[f] * per_row);
-      const int k = k128[f] * 128 + sub * 8;
-      if (item < n && row[f] < p.rows && k < p.H)
-        in[f].load(static_cast<const T*>(p.src) + static_cast<long long>(row[f]) * p.H + k);
+    for (int h = 0; h < 2; ++h)
+      if (there && k + 64 * h < p.H)
+        in[h].load(src + 64 * h);
       else
-        in[f].zero();
-    }
+        in[h].zero();
+    uint32_t code[2], packed[2];
 #pragma unroll
-    for (int f = 0; f < kFlight; ++f) {
-      if (((q + f * step) & ~1u) >= n) break;  // the same in the whole warp
-      float x[8];
-      in[f].floats(x);
-      float high = 0.0f;
-#pragma unroll
-      for (int i = 0; i < 8; ++i) high = fmaxf(high, fabsf(x[i]));
-      bool finite = true;
-#pragma unroll
-      for (int i = 0; i < 8; ++i) finite &= fabsf(x[i]) <= 3.402823466e38f;
-      high = fmaxf(high, __shfl_xor_sync(0xffffffffu, high, 1));
-      high = fmaxf(high, __shfl_xor_sync(0xffffffffu, high, 2));
-      const uint32_t ok = __ballot_sync(0xffffffffu, finite);
+    for (int h = 0; h < 2; ++h) {
+      uint32_t e = in[h].exponent();
+      e = max(e, __shfl_xor_sync(0xffffffffu, e, 1));
+      e = max(e, __shfl_xor_sync(0xffffffffu, e, 2));
       // The scale's exponent, biased: that of the largest value less 2; 255 (no
       // number) where a value is none.
-      const int e = static_cast<int>(__float_as_uint(high) >> 23);
-      uint32_t code = e > 2 ? e - 2 : 0;
-      if (((ok >> (lane & 28)) & 15u) != 15u) code = 255;
-      const float inv = __uint_as_float(code == 255 ? 0u : (254u - code) << 23);
-      uint32_t packed = 0;
+      code[h] = e == 255 ? 255u : max(e, 2u) - 2u;
+      const float inv = __uint_as_float(e == 255 ? 0u : (254u - code[h]) << 23);
+      float x[8];
+      in[h].floats(x);
+      packed[h] = 0;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) packed |= mx4_code2(x[2 * i] * inv, x[2 * i + 1] * inv) << (8 * i);
-      uint32_t scales = 0;
-#pragma unroll
-      for (int j = 0; j < 4; ++j)
-        scales |= __shfl_sync(0xffffffffu, code, (lane & 16) + 4 * j) << (8 * j);
-      const uint32_t t = row[f] / static_cast<uint32_t>(p.tile);
-      const int r = static_cast<int>(row[f] - t * p.tile), h = k128[f] & 1;
-      uint8_t* base = p.dst + (static_cast<size_t>(t) * p.KB + (k128[f] >> 1)) * stage;
-      const int chunk = h * 4 + (sub >> 2);
-      *reinterpret_cast<uint32_t*>(base + r * 128 + ((chunk ^ (r & 7)) << 4) + (sub & 3) * 4) = packed;
+      for (int i = 0; i < 4; ++i) {
+        const float2 y = __fmul2_rn(make_float2(x[2 * i], x[2 * i + 1]), make_float2(inv, inv));
+        packed[h] |= mx4_code2(y.x, y.y) << (8 * i);
+      }
+    }
+    uint32_t scales = code[0] | code[1] << 16;
+    scales |= __shfl_xor_sync(0xffffffffu, scales, 4) << 8;  // whole in the first four lanes
+    if (q < n) {
+      uint8_t* base = p.dst + (static_cast<size_t>(at.t) * p.KB + (at.k >> 1)) * stage;
+      const uint32_t half = at.k & 1, chunk = (half * 4 + (sub >> 2)) ^ (at.r & 7);
+      uint8_t* codes = base + at.r * 128 + (sub & 3) * 4;
+      *reinterpret_cast<uint32_t*>(codes + (chunk << 4)) = packed[0];
+      *reinterpret_cast<uint32_t*>(codes + ((chunk ^ 2) << 4)) = packed[1];
       if (sub == 0)
-        *reinterpret_cast<uint32_t*>(base + p.tile * 128 + (h * groups + (r >> 7)) * kMx4ScaleAtom +
-                                     (r & 31) * 16 + ((r >> 5) & 3) * 4) = scales;
-      const int k = k128[f] * 128 + sub * 8;
-      if (p.values && row[f] < p.rows && k < p.H) {
-        const float scale = __uint_as_float(code == 255 ? 0x7fc00000u : code ? code << 23 : 0x00400000u);
+        *reinterpret_cast<uint32_t*>(base + tile * 128 + (half * groups + (at.r >> 7)) * kMx4ScaleAtom +
+                                     (at.r & 31) * 16 + ((at.r >> 5) & 3) * 4) = scales;
+    }
+    if (there && p.values) {
+      __nv_bfloat16* out = p.values + static_cast<long long>(at.row) * p.H + k;
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        if (k + 64 * h >= p.H) break;
+        const float scale =
+            __uint_as_float(code[h] == 255 ? 0x7fc00000u : code[h] ? code[h] << 23 : 0x00400000u);
         uint32_t v[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          const float2 y = mx4_value2((packed >> (8 * i)) & 255u);
-          const __nv_bfloat162 b = __floats2bfloat162_rn(y.x * scale, y.y * scale);
+          const float2 y = __fmul2_rn(mx4_value2((packed[h] >> (8 * i)) & 255u), make_float2(scale, scale));
+          const __nv_bfloat162 b = __floats2bfloat162_rn(y.x, y.y);
           v[i] = *reinterpret_cast<const uint32_t*>(&b);
         }
-        __stcs(reinterpret_cast<uint4*>(p.values + static_cast<long long>(row[f]) * p.H + k),
-               make_uint4(v[0], v[1], v[2], v[3]));
+        __stcs(reinterpret_cast<uint4*>(out + 64 * h), make_uint4(v[0], v[1], v[2], v[3]));
       }
     }
+    at.move(by, per_row, tile);
   }
 }
 
