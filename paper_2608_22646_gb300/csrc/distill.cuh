@@ -36,8 +36,6 @@ struct DistillParams {
   long long ld_grad;
 };
 
-constexpr float kLn2 = 0.6931471805599453f;
-
 // Running maximum and sum of 2^(x - max).
 struct MaxSum {
   float m, s;

@@ -16,6 +16,7 @@
 namespace cai {
 
 constexpr float kRowLog2e = kLog2e;
+constexpr float kLn2 = 0.6931471805599453f;
 constexpr int kTopMax = 512;                     // K of cai_top_rows
 
 struct SampleParams {
@@ -229,50 +230,53 @@ __device__ __forceinline__ uint32_t push_noted(const C& c, const S& s, Noted not
 }
 
 // The first pass of a row that is looked through for at least `want` largest
-// elements (0: for the largest alone): f(vector) for every vector; returns the
-// floor.  A CTA alone looks during the pass itself, above a floor from the part of
-// the row that it keeps, and then through that part, above the final one: no second
-// pass over the rest.  looked: whether `noted` is complete.
+// elements (0: for the largest alone); returns the floor.  A CTA alone looks during
+// the pass itself, above a floor from the part of the row that it keeps, and then
+// through that part, above the final one: no second pass over the rest.  looked:
+// whether `noted` is complete; f(vector, ref) was then called once for every
+// vector, ref the largest element of the part kept.
 template <typename T, bool kCluster, typename C, typename F>
 __device__ __forceinline__ Floor load_row(C& c, const Slice<T, kCluster>& s, int want, bool look,
-                                          Noted& noted, bool& looked, F&& f) {
+                                          Noted& noted, bool& looked, float& ref, F&& f) {
   const float inf = __uint_as_float(0x7f800000u);
   float m = -inf;
   looked = false;
   if (!kCluster && look && s.keep > 0) {
-    load_part<4>(s, 0, s.keep, [&](int, const uint4& v) {
-      m = vec_max(v, m, T());
-      f(v);
-    });
+    load_part<4>(s, 0, s.keep, [&](int, const uint4& v) { m = vec_max(v, m, T()); });
     const int warps = static_cast<int>(blockDim.x >> 5);
     const uint32_t mine = warp_floor<T>(m, (want + warps - 1) / warps);
-    uint32_t* floors = reinterpret_cast<uint32_t*>(c.sh->wred[1]);
-    if ((threadIdx.x & 31) == 0) floors[threadIdx.x >> 5] = mine;
+    const uint32_t top = __reduce_max_sync(0xffffffffu, key_of<float>(m));
+    unsigned long long* found = c.sh->wred[1];
+    if ((threadIdx.x & 31) == 0) found[threadIdx.x >> 5] = (static_cast<unsigned long long>(top) << 32) | mine;
     __syncthreads();
-    const uint32_t key = __reduce_min_sync(0xffffffffu, floors[threadIdx.x & (warps - 1)]);
+    const unsigned long long w = found[threadIdx.x & (warps - 1)];
+    const uint32_t key = __reduce_min_sync(0xffffffffu, static_cast<uint32_t>(w));
+    ref = value_of_key<float>(__reduce_max_sync(0xffffffffu, static_cast<uint32_t>(w >> 32)));
     noted.low = Floor{0.0f, key}.low<T>();
     looked = key > 0;
+  }
+  if (looked) {
     load_part<4>(s, s.keep, s.n_vec, [&](int v, const uint4& q) {
       const float top = vec_max(q, -inf, T());
       m = max_nan(m, top);
-      if (looked && !(top < noted.low)) noted.set(v);
-      f(q);
+      if (!(top < noted.low)) noted.set(v);
+      f(q, ref);
     });
   } else {
-    load_part<4>(s, 0, s.n_vec, [&](int, const uint4& v) {
-      m = vec_max(v, m, T());
-      f(v);
-    });
+    load_part<4>(s, !kCluster && look ? s.keep : 0, s.n_vec, [&](int, const uint4& v) { m = vec_max(v, m, T()); });
   }
   load_ends(s, [&](int, const uint4& v) {
     m = vec_max(v, m, T());
-    f(v);
+    if (looked) f(v, ref);
   });
   c.begun();
   const Floor floor = row_floor<T>(c, m, want);
   noted.low = floor.low<T>();
   if (looked)
-    for_body<4>(s, threadIdx.x, s.keep, blockDim.x, [&](int v, const uint4& q) { noted.look<T>(v, q); });
+    for_body<4>(s, threadIdx.x, s.keep, blockDim.x, [&](int v, const uint4& q) {
+      noted.look<T>(v, q);
+      f(q, ref);
+    });
   return floor;
 }
 
@@ -577,9 +581,10 @@ __global__ void __launch_bounds__(512, kCluster ? 1 : 2)
 
   Noted noted(s.n_vec);
   bool looked;
+  float ref;
   const Floor floor = load_row<T, kCluster>(c, s, p.V <= kListMax ? 0 : want,
-                                            want > 0 && set.k > 0 && p.V > kListMax, noted, looked,
-                                            [](const uint4&) {});
+                                            want > 0 && set.k > 0 && p.V > kListMax, noted, looked, ref,
+                                            [](const uint4&, float) {});
   const float zmax = set.zmax = floor.zmax;
 
   if (!(fabsf(zmax) < inf) || greedy) {
@@ -743,43 +748,47 @@ __global__ void __launch_bounds__(512, kCluster ? 1 : 2)
   if (threadIdx.x == 0) sh.listed = sh.noted = 0;
   const float inf = __uint_as_float(0x7f800000u);
   const float scale = __fdiv_rn(kRowLog2e, p.temperature);
-  // The sum of 2^((z - m) scale).  A CTA alone takes it along in the first pass,
-  // relative to the thread's maximum so far.
+  // The sum of 2^((z - base) scale).  A CTA alone takes it along in the first pass,
+  // with base the largest element of the part that it keeps: one fused step, without
+  // a running maximum (2000 rows of 126464 bf16, K = 128: with one in each thread,
+  // which nearly every vector raises somewhere in a warp, 185 us; so 176).  x =
+  // z scale - fl(base scale) is off by that product's rounding, which comes off the
+  // sum's logarithm.
   float2 sum2 = make_float2(0.0f, 0.0f);
-  float m = -inf;
-  const auto add = [&](const uint4& q, float from) {
-    float z[kVec];
-    Row<T>::unpack(q, z);
-#pragma unroll
-    for (int e = 0; e < kVec; e += 2)
-      sum2 = __fadd2_rn(sum2, row_exp2_pair(z[e], z[e + 1], from, scale));
-  };
+  float base;
   Noted noted(s.n_vec);
   bool looked;
   const Floor floor = load_row<T, kCluster>(
-      c, s, p.V <= kListMax ? 0 : p.K, p.V > kListMax, noted, looked, [&](const uint4& q) {
-        if (kCluster) return;
-        const float top = vec_max(q, -inf, T());
-        if (!(top <= m)) {  // a new maximum, or NaN
-          const float f = m == -inf ? 0.0f : fast_exp2((m - top) * scale);
-          sum2 = make_float2(sum2.x * f, sum2.y * f);
-          m = top;
+      c, s, p.V <= kListMax ? 0 : p.K, p.V > kListMax, noted, looked, base, [&](const uint4& q, float ref) {
+        const float from = -__fmul_rn(ref, scale);
+        float z[kVec];
+        Row<T>::unpack(q, z);
+#pragma unroll
+        for (int e = 0; e < kVec; e += 2) {
+          const float2 x = __ffma2_rn(make_float2(z[e], z[e + 1]), make_float2(scale, scale), make_float2(from, from));
+          sum2 = __fadd2_rn(sum2, make_float2(fast_exp2(x.x), fast_exp2(x.y)));
         }
-        if (m != -inf) add(q, m);
       });
   const float zmax = floor.zmax;
   // A row of small size is listed whole; a NaN is above every floor.
   const bool listing = p.V <= kListMax || floor.key > 0;
   uint32_t pushed = 0;
-  if (kCluster || !looked) {
+  // Where base is far below the row's largest, or no number, the sum is taken again.
+  float off = 0.0f;
+  const bool summed = looked && !__syncthreads_or(!(sum2.x + sum2.y < 1.15e18f));
+  if (summed) {
+    off = -__fmaf_rn(base, scale, -__fmul_rn(base, scale));
+  } else {
+    base = zmax;
     sum2 = make_float2(0.0f, 0.0f);
     for_slice<4>(s, [&](int v, const uint4& q) {
-      add(q, zmax);
-      if (listing) noted.look<T>(v, q);
+      float z[kVec];
+      Row<T>::unpack(q, z);
+#pragma unroll
+      for (int e = 0; e < kVec; e += 2)
+        sum2 = __fadd2_rn(sum2, row_exp2_pair(z[e], z[e + 1], base, scale));
+      if (listing && !looked) noted.look<T>(v, q);
     });
-  } else {
-    const float f = m == -inf ? 0.0f : fast_exp2((m - zmax) * scale);
-    sum2 = make_float2(sum2.x * f, sum2.y * f);
   }
   if (listing) pushed = push_noted<T>(c, s, noted, [](float) {});
   float sum = __uint_as_float(static_cast<uint32_t>(
@@ -813,7 +822,7 @@ __global__ void __launch_bounds__(512, kCluster ? 1 : 2)
     p.index[static_cast<long long>(r) * p.K + i] = candidate_index(x);
   }
   if (threadIdx.x == 0)
-    p.lse[r] = fabsf(zmax) < inf ? __fdiv_rn(zmax, p.temperature) + logf(sum) : zmax;
+    p.lse[r] = fabsf(zmax) < inf ? __fdiv_rn(base, p.temperature) + (logf(sum) + off * kLn2) : zmax;
 }
 
 }  // namespace cai
