@@ -95,6 +95,47 @@ __device__ __forceinline__ float vec_max(const uint4& v, float m, __nv_bfloat16)
   return max_nan(m, max_nan(__uint_as_float(r << 16), __uint_as_float(r & 0xffff0000u)));
 }
 
+// The largest of a thread's elements, in parts: each part of a vector has a maximum
+// of its own, NaN kept.
+template <typename T>
+struct Maxima;
+template <>
+struct Maxima<float> {
+  static constexpr int kParts = 2;
+  float a, b;
+  __device__ __forceinline__ Maxima() : a(-__builtin_huge_valf()), b(a) {}
+  // Adds a vector; returns its largest element.
+  __device__ __forceinline__ float add(const uint4& v) {
+    const float x = max_nan(__uint_as_float(v.x), __uint_as_float(v.y));
+    const float y = max_nan(__uint_as_float(v.z), __uint_as_float(v.w));
+    a = max_nan(a, x);
+    b = max_nan(b, y);
+    return max_nan(x, y);
+  }
+  __device__ __forceinline__ float part(int i) const { return i ? b : a; }
+  __device__ __forceinline__ float all() const { return max_nan(a, b); }
+};
+template <>
+struct Maxima<__nv_bfloat16> {
+  static constexpr int kParts = 4;
+  uint32_t a, b;
+  __device__ __forceinline__ Maxima() : a(0xff80ff80u), b(a) {}
+  static __device__ __forceinline__ float of(uint32_t r) {
+    return max_nan(__uint_as_float(r << 16), __uint_as_float(r & 0xffff0000u));
+  }
+  __device__ __forceinline__ float add(const uint4& v) {
+    const uint32_t x = max2_nan(v.x, v.y), y = max2_nan(v.z, v.w);
+    a = max2_nan(a, x);
+    b = max2_nan(b, y);
+    return of(max2_nan(x, y));
+  }
+  __device__ __forceinline__ float part(int i) const {
+    const uint32_t r = i & 2 ? b : a;
+    return __uint_as_float(i & 1 ? r & 0xffff0000u : r << 16);
+  }
+  __device__ __forceinline__ float all() const { return of(max2_nan(a, b)); }
+};
+
 // Order of the logits as whole numbers: rises with the value, -0 and +0 are the
 // same, NaN is above +inf.  bf16 values differ in the upper 16 bits alone.
 template <typename T>
@@ -742,20 +783,37 @@ __device__ __forceinline__ Told tell(const C& c, bool mine, uint32_t a, uint32_t
 
 // ------------------------------------------------------------- candidates --
 
-// A key with at least `count` elements of this warp's at or above it: the
-// count-th largest of the lanes' maxima (each stands for an element), its lower
-// 16 bits cleared in 32-bit keys; 0 where count is above 32.
-template <typename T>
-__device__ __forceinline__ uint32_t warp_floor(float lane_max, int count) {
-  constexpr int kDrop = Row<T>::kKeyBits - 16;
-  const uint32_t key = key_of<T>(lane_max) >> kDrop;
+// The count-th largest of kN 16-bit keys of each lane of a warp; 0 where count is
+// above their number.
+template <int kN>
+__device__ __forceinline__ uint32_t warp_select(const uint32_t (&key)[kN], int count) {
   uint32_t found = 0;
-#pragma unroll
+#pragma unroll(kN == 1 ? 16 : 1)
   for (int bit = 15; bit >= 0; --bit) {
     const uint32_t t = found | (1u << bit);
-    if (__popc(__ballot_sync(0xffffffffu, key >= t)) >= count) found = t;
+    int n = 0;
+#pragma unroll
+    for (int i = 0; i < kN; ++i) n += __popc(__ballot_sync(0xffffffffu, key[i] >= t));
+    if (n >= count) found = t;
   }
-  return found << kDrop;
+  return found;
+}
+// A key with at least `count` elements of this warp's at or above it (0: none is
+// known), its lower 16 bits cleared in 32-bit keys: the count-th largest of the
+// lanes' maxima, or of their parts' where that lies below the middle of the lanes
+// (2048 rows of 4000 bf16, K = 256: the 32nd of 32 250 us, of 128 80; 2000 rows of
+// 126464, K = 128: the 8th of 32 177 us, of 128 184).
+template <typename T>
+__device__ __forceinline__ uint32_t warp_floor(const Maxima<T>& m, int count) {
+  constexpr int kDrop = Row<T>::kKeyBits - 16, kParts = Maxima<T>::kParts;
+  if (count <= 16) {
+    const uint32_t key[1] = {key_of<T>(m.all()) >> kDrop};
+    return warp_select(key, count) << kDrop;
+  }
+  uint32_t key[kParts];
+#pragma unroll
+  for (int i = 0; i < kParts; ++i) key[i] = key_of<T>(m.part(i)) >> kDrop;
+  return warp_select(key, count) << kDrop;
 }
 
 // Order of candidates: falling key, then rising index.
@@ -860,11 +918,12 @@ struct RowPlan {
 // CTA on an SM beside its fixed_smem.
 __host__ __forceinline__ RowPlan row_plan(int M, int V, int elem, int sms, size_t limit,
                                           size_t fixed_smem, size_t (*extra)(int)) {
-  // A cluster: as few CTAs as keep a slice within 72 KiB, up to four while the
+  // A cluster: as few CTAs as keep a slice within 84 KiB, two to an SM (64 rows of
+  // 152064 bf16, K = 64: 4 CTAs 16.6 us, 8 26.6), up to four while the
   // grid leaves SMs idle and slices stay long; 256 threads, whose reductions and
   // barriers cost less (one row of 126464 bf16, sampled: 4 CTAs of 256 threads
   // 15.4 us, of 512 16.5, 8 of 256 16.4, 8 of 512 22).
-  constexpr size_t kSliceTarget = 72 * 1024;
+  constexpr size_t kSliceTarget = 84 * 1024;
   int c = 1;
   while (c < kRowMaxCluster && row_slice_bytes(V, c, elem) > kSliceTarget) c *= 2;
   while (c < 4 && static_cast<long long>(M) * c * 2 <= sms && V / c > 4096) c *= 2;

@@ -66,12 +66,16 @@ struct Floor {
     return v == v ? v : __uint_as_float(0xff800000u);
   }
 };
+// full: the warps of a CTA whose lanes all have elements, one at least; where there
+// are fewer than warps, they alone find it.
 template <typename T, typename C>
-__device__ __forceinline__ Floor row_floor(C& c, float thread_max, int want) {
-  const int warps = c.ctas() * static_cast<int>(blockDim.x >> 5);
-  const uint32_t floor = want > 0 ? warp_floor<T>(thread_max, (want + warps - 1) / warps) : 0u;
+__device__ __forceinline__ Floor row_floor(C& c, const Maxima<T>& m, int want, int full) {
+  const int warps = c.ctas() * full;
+  uint32_t floor = 0;
+  if (want > 0)
+    floor = static_cast<int>(threadIdx.x >> 5) < full ? warp_floor<T>(m, (want + warps - 1) / warps) : 0xffffffffu;
   // Both as one value: the largest key, and the smallest floor as its complement.
-  const uint32_t top = __reduce_max_sync(0xffffffffu, key_of<float>(thread_max));
+  const uint32_t top = __reduce_max_sync(0xffffffffu, key_of<float>(m.all()));
   RowShared* sh = c.sh;
   const int lane = threadIdx.x & 31, n = blockDim.x >> 5;
   if (lane == 0) sh->wred[0][threadIdx.x >> 5] = (static_cast<unsigned long long>(top) << 32) | floor;
@@ -238,14 +242,13 @@ __device__ __forceinline__ uint32_t push_noted(const C& c, const S& s, Noted not
 template <typename T, bool kCluster, typename C, typename F>
 __device__ __forceinline__ Floor load_row(C& c, const Slice<T, kCluster>& s, int want, bool look,
                                           Noted& noted, bool& looked, float& ref, F&& f) {
-  const float inf = __uint_as_float(0x7f800000u);
-  float m = -inf;
+  const int warps = static_cast<int>(blockDim.x >> 5);
+  Maxima<T> m;
   looked = false;
   if (!kCluster && look && s.keep > 0) {
-    load_part<4>(s, 0, s.keep, [&](int, const uint4& v) { m = vec_max(v, m, T()); });
-    const int warps = static_cast<int>(blockDim.x >> 5);
+    load_part<4>(s, 0, s.keep, [&](int, const uint4& v) { m.add(v); });
     const uint32_t mine = warp_floor<T>(m, (want + warps - 1) / warps);
-    const uint32_t top = __reduce_max_sync(0xffffffffu, key_of<float>(m));
+    const uint32_t top = __reduce_max_sync(0xffffffffu, key_of<float>(m.all()));
     unsigned long long* found = c.sh->wred[1];
     if ((threadIdx.x & 31) == 0) found[threadIdx.x >> 5] = (static_cast<unsigned long long>(top) << 32) | mine;
     __syncthreads();
@@ -257,20 +260,20 @@ __device__ __forceinline__ Floor load_row(C& c, const Slice<T, kCluster>& s, int
   }
   if (looked) {
     load_part<4>(s, s.keep, s.n_vec, [&](int v, const uint4& q) {
-      const float top = vec_max(q, -inf, T());
-      m = max_nan(m, top);
-      if (!(top < noted.low)) noted.set(v);
+      if (!(m.add(q) < noted.low)) noted.set(v);
       f(q, ref);
     });
   } else {
-    load_part<4>(s, !kCluster && look ? s.keep : 0, s.n_vec, [&](int, const uint4& v) { m = vec_max(v, m, T()); });
+    load_part<4>(s, !kCluster && look ? s.keep : 0, s.n_vec, [&](int, const uint4& v) { m.add(v); });
   }
   load_ends(s, [&](int, const uint4& v) {
-    m = vec_max(v, m, T());
+    m.add(v);
     if (looked) f(v, ref);
   });
   c.begun();
-  const Floor floor = row_floor<T>(c, m, want);
+  // (slices of several CTAs are long)
+  const int full = c.ctas() > 1 ? warps : max(1, min(warps, s.last / 32));
+  const Floor floor = row_floor<T>(c, m, want, full);
   noted.low = floor.low<T>();
   if (looked)
     for_body<4>(s, threadIdx.x, s.keep, blockDim.x, [&](int v, const uint4& q) {
@@ -582,8 +585,7 @@ __global__ void __launch_bounds__(512, kCluster ? 1 : 2)
   Noted noted(s.n_vec);
   bool looked;
   float ref;
-  const Floor floor = load_row<T, kCluster>(c, s, p.V <= kListMax ? 0 : want,
-                                            want > 0 && set.k > 0 && p.V > kListMax, noted, looked, ref,
+  const Floor floor = load_row<T, kCluster>(c, s, want, want > 0 && set.k > 0, noted, looked, ref,
                                             [](const uint4&, float) {});
   const float zmax = set.zmax = floor.zmax;
 
@@ -759,7 +761,7 @@ __global__ void __launch_bounds__(512, kCluster ? 1 : 2)
   Noted noted(s.n_vec);
   bool looked;
   const Floor floor = load_row<T, kCluster>(
-      c, s, p.V <= kListMax ? 0 : p.K, p.V > kListMax, noted, looked, base, [&](const uint4& q, float ref) {
+      c, s, p.K, true, noted, looked, base, [&](const uint4& q, float ref) {
         const float from = -__fmul_rn(ref, scale);
         float z[kVec];
         Row<T>::unpack(q, z);
@@ -770,7 +772,7 @@ __global__ void __launch_bounds__(512, kCluster ? 1 : 2)
         }
       });
   const float zmax = floor.zmax;
-  // A row of small size is listed whole; a NaN is above every floor.
+  // (a NaN is above every floor)
   const bool listing = p.V <= kListMax || floor.key > 0;
   uint32_t pushed = 0;
   // Where base is far below the row's largest, or no number, the sum is taken again.

@@ -207,3 +207,54 @@ def test_temperatures_beyond_32_bits_are_refused(temperature):
     v.zero_(), i.zero_()
     with pytest.raises(cai.CaiError):
         cai.cai_distill_loss(z, v, i, loss, stats, temperature=temperature)
+
+
+@pytest.mark.parametrize("M", [2, MANY])
+@pytest.mark.parametrize("V,K", [(33, 1), (300, 200), (1000, 8), (1000, 256), (2047, 500), (2049, 256), (4000, 512),
+                                 (45001, 256)])
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_records_of_short_rows_and_many_entries(M, V, K, dtype):
+    z = rows_of(M, V, dtype, V + K, pad=3, offset=1)
+    z[1, V // 2:] = -float("inf")
+    v, i, _ = top(z, K)
+    zz = z.double().cpu().numpy()
+    for r in range(0, M, 7):
+        order = ref.order_of(zz[r])[:K]
+        assert (i[r] == order).all() and (v[r] == zz[r][order]).all()
+
+
+@pytest.mark.parametrize("V", [700, 1500, 2048])
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_short_rows_sampled(V, dtype):
+    z = rows_of(MANY, V, dtype, V, pad=1, offset=3)
+    z[4, V // 3:] = -float("inf")
+    u = torch.rand(MANY, generator=torch.Generator().manual_seed(V)).cuda()
+    T, k, p, m = settings(MANY, V)
+    token, prob = draw(z, u, **as_kw(T, k, p, m))
+    assert check_sampled(z, u, token, prob, T, k, p, m) >= MANY // 2
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_records_whose_rows_begin_far_below_their_largest(dtype):
+    """The first part of a row says little of the rest.  lse: within 6e-6 + 2e-7
+    of its size, as for other rows."""
+    V, K = 60001, 5
+    z = rows_of(MANY, V, dtype, 11, pad=7, offset=1)
+    first = 3 * V // 4
+    z[0, first + 5] = 30.0
+    z[1, first + 6] = 90.0
+    z[2, first + 7] = 900.0
+    z[3, :first] = -float("inf")
+    z[4, :first] = torch.finfo(dtype).min
+    z[5] -= 3000.0
+    z[6, :first] -= 80.0
+    z[7] = torch.finfo(dtype).min
+    v, i, l = top(z, K, 1.25)
+    zz = z[:16].double().cpu().numpy()
+    for r in range(16):
+        order = ref.order_of(zz[r])[:K]
+        assert (i[r] == order).all() and (v[r] == zz[r][order]).all()
+        if r != 7:
+            want = ref.softmax_lse(zz[r] / 1.25)
+            assert abs(l[r] - want) <= 6e-6 + 2e-7 * abs(want)
+    assert abs(l[7] / (zz[7][0] / 1.25) - 1) < 2e-7
