@@ -22,7 +22,6 @@
 
 namespace cai {
 
-constexpr int kMx4Block = 32;          // values per scale
 constexpr int kMx4K = 256;             // values of H per stage: 128 bytes of codes
 constexpr int kMx4MaxTile = 208;       // vocabulary rows per tile, at most
 constexpr int kMx4RowTile = 128;       // rows of the step per tile (MMA M)
@@ -465,6 +464,10 @@ __device__ __forceinline__ bool mx4_issue_all(const Mx4Params& p, int n_tiles, u
   return true;
 }
 
+// Up to 128 rows: the rows' codes as A (M = 128, of which a step owns few), a tile
+// of the vocabulary as B, one CTA on an SM over tiles; two accumulators, so that a
+// tile leaves while the next is summed.  Bound by W's bytes: 1 row, V = 126464, H =
+// 4096, 47 us with the packing launch, 41 at the copy's rate of 275 MB; 128 rows 53.
 template <typename T>
 __global__ void __launch_bounds__(kMx4Threads, 1) mx4_logits_kernel(const Mx4Params p) {
   extern __shared__ uint8_t smem_raw[];
@@ -579,9 +582,10 @@ __global__ void __launch_bounds__(kMx4Threads, 1) mx4_logits_kernel(const Mx4Par
 // More than 128 rows: CTA pairs (cta_group::2) on tiles of 256 rows, each CTA with
 // its 128 rows and half of the tile's W.  One CTA on 128 rows takes 46 KiB into its
 // shared memory for MMAs of 0.22 us, more than an SM's share of L2 gives (2048 x
-// 126464 x 4096: 105 KB/us, 459 us); a pair's CTA takes 32 KiB for as much (409).
-// The packed weight and rows are seen as rows of 128 bytes for the copies, which
-// complete on the even CTA's barriers.
+// 126464 x 4096: 105 KB/us, 459 us); a pair's CTA takes 32 KiB for as much (409 to
+// 421, the tensor pipe busy 51 % of the time; bound by the scales' copies, which
+// take turns with the MMAs).  The packed weight and rows are seen as rows of 128
+// bytes for the copies, which complete on the even CTA's barriers.
 struct Mx4PairMaps {
   CUtensorMap rows, w, scales;  // boxes: a row tile's stage, half a tile's codes, its scales
 };

@@ -927,7 +927,12 @@ __host__ __forceinline__ RowPlan row_plan(int M, int V, int elem, int sms, size_
   int c = 1;
   while (c < kRowMaxCluster && row_slice_bytes(V, c, elem) > kSliceTarget) c *= 2;
   while (c < 4 && static_cast<long long>(M) * c * 2 <= sms && V / c > 4096) c *= 2;
-  if (c == 1 || M < sms)
+  // Clusters that fill the SMs, two CTAs each, once; of more rows each goes to a CTA
+  // alone (126464 bf16, K = 64: 64 rows 16.9 us either way, 90 23.8 and 17.0, 152 34
+  // and 18, 304 58 and 24; loss and gradient: 64 rows 17 and 23, 90 27 and 23), but
+  // half as many again of the longest, which take one CTA long (152064 float32, loss
+  // and gradient: 50 rows 31 and 39, 100 47 and 46; K = 64: 25 and 29, 42 and 29).
+  if (c == 1 || static_cast<long long>(M) * c <= (c == kRowMaxCluster ? 3ll : 2ll) * sms)
     return RowPlan{c, 256, 0, row_slice_bytes(V, c, elem) + extra(row_chunk(V, c))};
   // Alone, two on an SM: what shared memory that leaves, in whole rounds of the
   // CTA's threads.

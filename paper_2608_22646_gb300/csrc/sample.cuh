@@ -187,32 +187,47 @@ struct Noted {
 // After the pass, pushes the elements that are not below the floor, each thread
 // some of the noted vectors of all, and calls f(value) for each.  Returns how many
 // this thread pushed; more than the list holds if there were too many vectors.
+// again: they were noted above a lower floor than the final one; should they be too
+// many, the row is looked through once more (500 rows of 152064 float32, K = 64: 103
+// us; searching for the K-th instead 199).
 template <typename T, typename C, typename S, typename F>
-__device__ __forceinline__ uint32_t push_noted(const C& c, const S& s, Noted noted, F&& f) {
+__device__ __forceinline__ uint32_t push_noted(const C& c, const S& s, Noted noted, bool again, F&& f) {
   RowShared* sh = c.sh;
   const int nt = blockDim.x, tid = threadIdx.x;
   const int first = S::kKept ? 0 : s.first, last = S::kKept ? s.n_vec : s.last;
   const int span = (1 << noted.shift) / nt;  // rounds of a bit
   const int end = S::kKept ? -1 : s.end_of(tid);
-  const uint32_t mine = __popcll(noted.bits) * span + (end >= 0);
-  if (mine) {
-    uint32_t at = atomicAdd(&sh->noted, mine);
-    if (end >= 0 && at < kListMax) sh->note[at++] = static_cast<uint32_t>(end);
+  uint32_t n;
 #pragma unroll 1
-    while (noted.bits) {
-      const int k = __ffsll(noted.bits) - 1;
-      noted.bits &= noted.bits - 1;
+  for (;;) {
+    const uint32_t mine = __popcll(noted.bits) * span + (end >= 0);
+    if (mine) {
+      uint32_t at = atomicAdd(&sh->noted, mine);
+      if (end >= 0 && at < kListMax) sh->note[at++] = static_cast<uint32_t>(end);
+      unsigned long long bits = noted.bits;
 #pragma unroll 1
-      for (int j = 0; j < span; ++j, ++at) {
-        // (what an end set stands for one of the thread's other vectors)
-        const int v = (k * span + j) * nt + tid;
-        if (at < kListMax) sh->note[at] = v >= first && v < last ? static_cast<uint32_t>(v) : ~0u;
+      while (bits) {
+        const int k = __ffsll(bits) - 1;
+        bits &= bits - 1;
+#pragma unroll 1
+        for (int j = 0; j < span; ++j, ++at) {
+          // (what an end set stands for one of the thread's other vectors)
+          const int v = (k * span + j) * nt + tid;
+          if (at < kListMax) sh->note[at] = v >= first && v < last ? static_cast<uint32_t>(v) : ~0u;
+        }
       }
     }
+    __syncthreads();
+    n = sh->noted;
+    if (n <= kListMax) break;
+    if (!again) return kListMax + 1;
+    again = false;
+    __syncthreads();  // read by all
+    if (tid == 0) sh->noted = 0;
+    noted.bits = 0;
+    for_slice<4>(s, [&](int v, const uint4& q) { noted.look<T>(v, q); });
+    __syncthreads();
   }
-  __syncthreads();
-  const uint32_t n = sh->noted;
-  if (n > kListMax) return kListMax + 1;
   uint32_t pushed = 0;
 #pragma unroll 1
   for (uint32_t k = tid; k < n; k += nt) {
@@ -397,8 +412,9 @@ __device__ __noinline__ Kept keep_weight(C& c, const S s, const Bracket br, unsi
           const float z = br.low + (static_cast<float>(b) + 0.5f) * width;
           return static_cast<unsigned long long>(static_cast<float>(n) * kWeightUnit * share(-1, z, z).x);
         });
-    int bin = l.bin;
-    const int around = 4 * l.count < kListMax ? 1 : 0;  // parts to either side
+    // (-1: the guesses add up to less than is wanted; then it is the lowest part)
+    int bin = max(l.bin, 0);
+    const int around = l.bin >= 0 && 4 * l.count < kListMax ? 1 : 0;  // parts to either side
 #pragma unroll 1
     for (int turn = 0; turn < 4 && bin >= 0 && bin < kBins; ++turn) {
       if (threadIdx.x == 0) c.sh->listed = 0;
@@ -550,9 +566,18 @@ __device__ __noinline__ void sample_candidates(RowShared* sh, const SampleParams
   draw_listed<T>(sh, p, r, static_cast<int>(n_kept), set);
 }
 
-// Candidates asked for where only the weight limits what is kept.
+// Candidates asked for where only the weight limits what is kept (64 rows of 50003
+// float32, top-p, where a nucleus has some dozens of tokens: 64 18.5 us, 128 20.5,
+// 256 25; one that reaches past the listed ones takes 40 to 75 in keep_weight).
 constexpr int kNucleusWant = 128;
 
+// One pass over a row for its maximum and a floor, one for the weights (top-k needs
+// none) and the candidates; few rows keep the row in shared memory, so HBM is read
+// once.  Few rows are bound by the chain of reductions between the CTAs (one row of
+// 126464 bf16 15 us, of which the host's call 8; 64 of 50003 float32 20 to 41), many
+// by the instructions of the weights, 75 to 130 for 16 bytes, and by loads that two
+// CTAs on an SM do not wholly hide: 2048 rows of 126464 bf16, settings of all kinds,
+// 314 us, 1.65 TB/s.
 template <typename T, bool kCluster>
 __global__ void __launch_bounds__(512, kCluster ? 1 : 2)
     sample_rows_kernel(const __grid_constant__ SampleParams p, int ctas) {
@@ -659,7 +684,7 @@ __global__ void __launch_bounds__(512, kCluster ? 1 : 2)
       });
     }
     if (listing)
-      pushed = push_noted<T>(c, s, noted, [&](float z) {
+      pushed = push_noted<T>(c, s, noted, looked, [&](float z) {
         if (set.k == 0) listed_mass += set.weight(z);
       });
     const unsigned long long sums[3] = {sum.sum(n), listed_mass, pushed};
@@ -734,6 +759,11 @@ struct AddFloatOp {  // on the bits of floats, in a fixed order
   }
 };
 
+// The maximum and a floor, the sum of exponentials, the candidates sorted.  32 rows
+// of 152064 bf16, K = 64: 15 us, bound by latency and the host's call; 2000 of
+// 126464, K = 128: 177 us, 2.9 TB/s of 506 MB read once.  The SMs issue on 55 % of
+// the cycles: 60 instructions for 16 bytes and some 20000 a row for floors, pushes
+// and the sort, whose barriers and loads two CTAs on an SM hide in part only.
 template <typename T, bool kCluster>
 __global__ void __launch_bounds__(512, kCluster ? 1 : 2)
     top_rows_kernel(const __grid_constant__ TopParams p, int ctas) {
@@ -792,7 +822,7 @@ __global__ void __launch_bounds__(512, kCluster ? 1 : 2)
       if (listing && !looked) noted.look<T>(v, q);
     });
   }
-  if (listing) pushed = push_noted<T>(c, s, noted, [](float) {});
+  if (listing) pushed = push_noted<T>(c, s, noted, looked, [](float) {});
   float sum = __uint_as_float(static_cast<uint32_t>(
       cta_reduce(&sh, __float_as_uint(sum2.x + sum2.y), AddFloatOp(), 1)));
   const unsigned long long v[2] = {

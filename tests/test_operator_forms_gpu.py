@@ -258,3 +258,23 @@ def test_records_whose_rows_begin_far_below_their_largest(dtype):
             want = ref.softmax_lse(zz[r] / 1.25)
             assert abs(l[r] - want) <= 6e-6 + 2e-7 * abs(want)
     assert abs(l[7] / (zz[7][0] / 1.25) - 1) < 2e-7
+
+
+@pytest.mark.parametrize("V,dtype", [(152064, F32), (131100, F32), (200003, BF16)])
+def test_long_rows_each_to_one_cta(V, dtype):
+    """Rows whose kept part is a small share of them."""
+    M, K = 160, 200
+    z = rows_of(M, V, dtype, V, pad=5, offset=1)
+    v, i, _ = top(z, K)
+    for r in range(0, M, 23):
+        zz = z[r].double().cpu().numpy()
+        order = ref.order_of(zz)[:K]
+        assert (i[r] == order).all() and (v[r] == zz[order]).all()
+    u = torch.rand(M, generator=torch.Generator().manual_seed(V)).cuda()
+    T, k, p, m = settings(M, V)
+    p[:20], k[:20] = 0.999, 0       # wide nuclei, their weight nearly the whole
+    token, prob = draw(z, u, **as_kw(T, k, p, m))
+    part = slice(0, 30)
+    t2, p2 = draw(z[part], u[part], **as_kw(T[part], k[part], p[part], m[part]))  # by clusters
+    assert (t2 == token[part]).all() and (p2 == prob[part]).all()
+    assert check_sampled(z[:60], u[:60], token[:60], prob[:60], T[:60], k[:60], p[:60], m[:60]) >= 30
