@@ -36,15 +36,21 @@ struct DistillParams {
   long long ld_grad;
 };
 
-// Running maximum and sum of 2^(x - max).
+// Running maximum of logits and sum of 2^((z - max) c2).  The maximum is a logit, and
+// differences are taken before the product: relative to a rounded max c2, the
+// exponent of the maximum itself would be that product's rounding error, hundreds
+// where |max c2| passes 2^31 and 10^30 at a type's lowest value.
 struct MaxSum {
   float m, s;
 };
-__device__ __forceinline__ MaxSum merge(MaxSum a, MaxSum b) {
+__device__ __forceinline__ float share_of(float z, float from, float c2) {
+  return fast_exp2(__fmul_rn(__fsub_rn(z, from), c2));
+}
+__device__ __forceinline__ MaxSum merge(MaxSum a, MaxSum b, float c2) {
   const float m = fmaxf(a.m, b.m);
   // -inf on both sides: no element yet.
-  const float ea = a.m == m ? 1.0f : fast_exp2(a.m - m);
-  const float eb = b.m == m ? 1.0f : fast_exp2(b.m - m);
+  const float ea = a.m == m ? 1.0f : share_of(a.m, m, c2);
+  const float eb = b.m == m ? 1.0f : share_of(b.m, m, c2);
   return MaxSum{m, a.s * ea + b.s * eb};
 }
 __device__ __forceinline__ unsigned long long bits_of(MaxSum a) {
@@ -55,9 +61,10 @@ __device__ __forceinline__ MaxSum max_sum_of(unsigned long long b) {
                 __uint_as_float(static_cast<uint32_t>(b >> 32))};
 }
 struct MaxSumOp {
+  float c2;
   __device__ __forceinline__ unsigned long long operator()(unsigned long long a,
                                                            unsigned long long b) const {
-    return bits_of(merge(max_sum_of(a), max_sum_of(b)));
+    return bits_of(merge(max_sum_of(a), max_sum_of(b), c2));
   }
 };
 
@@ -239,25 +246,32 @@ __global__ void __launch_bounds__(512, kCluster ? 1 : 2)
       if (speaks >> j & 1u) rec.q[k] = rec.token_q[k];
   }
 
-  // The sums of 2^x, x = z log2(e) / tau, over the record and over the rest, each
-  // relative to a reference of its own: its maximum, and in the backward call
-  // the logarithm that the forward call left.  The backward call adds them up
-  // again, since a logarithm of about 20 in fp32 holds p to 1e-6 only.
+  // The sums of 2^(z log2(e) / tau) over the record and over the rest, each relative
+  // to a logit of its own: its maximum, and in the backward call the one that the
+  // forward call's logarithm stands for.  The backward call adds them up again, since
+  // a logarithm of about 20 in fp32 holds p to 1e-6 only; where the logarithms are so
+  // large (or none) that their rounding is no small factor, it looks for the maxima.
   const float c2 = __fdiv_rn(kRowLog2e, p.tau);
   MaxSum in{-inf, 0.0f}, out{-inf, 0.0f};
+  bool known = false;
   if (backward) {
-    in.m = p.stats[2ll * r] * kRowLog2e;
-    out.m = p.stats[2ll * r + 1] * kRowLog2e;
+    constexpr float kMost = 1048576.0f;  // 2^20: rounded by 2^-5
+    const float l0 = p.stats[2ll * r], l1 = p.stats[2ll * r + 1];
+    const float m0 = l0 * p.tau, m1 = l1 * p.tau;
+    known = fabsf(l0) < kMost && fabsf(l1) < kMost && fabsf(m0) < 1e37f && fabsf(m1) < 1e37f;
+    if (known) {
+      in.m = m0;
+      out.m = m1;
+    }
   }
 #pragma unroll 1
   for (int k = tid, j = 0; k < p.K; k += nt, ++j)
     if (speaks >> j & 1u) {
-      if (backward) {
-        in.s += fast_exp2(fmaf(rec.z[k], c2, -in.m));
-      } else {
-        const float x = rec.z[k] * c2;
-        in = merge(in, MaxSum{x, x == -inf ? 0.0f : fast_exp2(fmaf(rec.z[k], c2, -x))});
-      }
+      const float z = rec.z[k];
+      if (known)
+        in.s += share_of(z, in.m, c2);
+      else  // (z - z: NaN for an infinity)
+        in = merge(in, MaxSum{z, z == -inf ? 0.0f : 1.0f + (z - z)}, c2);
     }
   load_slice<4>(s, [&](int v, const uint4& q) {
     float z[kVec];
@@ -274,27 +288,20 @@ __global__ void __launch_bounds__(512, kCluster ? 1 : 2)
     } else {
       m = vec_max(q, -inf, T());
     }
-    if (!backward) {
-      m *= c2;
-      if (!(m <= out.m)) {  // a new maximum, or NaN
-        out.s = out.m == -inf ? 0.0f : out.s * fast_exp2(out.m - m);
-        out.m = m;
-      }
+    if (!known && !(m <= out.m)) {  // a new maximum, or NaN
+      out.s = out.m == -inf ? 0.0f : out.s * share_of(out.m, m, c2);
+      out.m = m;
     }
     if (out.m != -inf) {
       float2 e2 = make_float2(0.0f, 0.0f);
 #pragma unroll
-      for (int e = 0; e < kVec; e += 2) {
-        const float2 x = __ffma2_rn(make_float2(z[e], z[e + 1]), make_float2(c2, c2),
-                                    make_float2(-out.m, -out.m));
-        e2 = __fadd2_rn(e2, make_float2(fast_exp2(x.x), fast_exp2(x.y)));
-      }
+      for (int e = 0; e < kVec; e += 2) e2 = __fadd2_rn(e2, row_exp2_pair(z[e], z[e + 1], out.m, c2));
       out.s += e2.x + e2.y;
     }
   });
   c.begun();
-  out = max_sum_of(cta_reduce(&sh, bits_of(out), MaxSumOp()));
-  in = max_sum_of(cta_reduce(&sh, bits_of(in), MaxSumOp(), 1));
+  out = max_sum_of(cta_reduce(&sh, bits_of(out), MaxSumOp{c2}));
+  in = max_sum_of(cta_reduce(&sh, bits_of(in), MaxSumOp{c2}, 1));
   {
     const unsigned long long mine[2] = {bits_of(out), bits_of(in)};
     const Parts parts = cluster_exchange(c, mine);
@@ -302,14 +309,14 @@ __global__ void __launch_bounds__(512, kCluster ? 1 : 2)
     in = max_sum_of(parts.of(1)[0]);
 #pragma unroll 1
     for (int q = 1; q < c.ctas(); ++q) {
-      out = merge(out, max_sum_of(parts.of(0)[q]));
-      in = merge(in, max_sum_of(parts.of(1)[q]));
+      out = merge(out, max_sum_of(parts.of(0)[q]), c2);
+      in = merge(in, max_sum_of(parts.of(1)[q]), c2);
     }
   }
-  const MaxSum all = merge(out, in);
+  const MaxSum all = merge(out, in, c2);
   const float ref = out.m == -inf ? 0.0f : out.m;
-  const float log2_all = log2f(all.s);
   if (!backward) {
+    const float log_all = logf(all.s);
     float part = 0.0f;
 #pragma unroll 1
     for (int k = tid; k < p.K; k += nt) {
@@ -317,7 +324,7 @@ __global__ void __launch_bounds__(512, kCluster ? 1 : 2)
       if (at >= 0 && s.holds(at)) {
         const float q = expf(rec.logq[k]);
         if (q > 0.0f)
-          part += q * (rec.logq[k] - (fmaf(rec.z[k], c2, -all.m) - log2_all) * kLn2);
+          part += q * (rec.logq[k] - (__fdiv_rn(rec.z[k] - all.m, p.tau) - log_all));
       }
     }
     part = cta_float(rec.scratch, part, add_op);
@@ -328,11 +335,11 @@ __global__ void __launch_bounds__(512, kCluster ? 1 : 2)
       float kl = 0.0f;
 #pragma unroll 1
       for (int q = 0; q < c.ctas(); ++q) kl += rec.loss_part[q];
-      const float log_rest = ((out.m - all.m) + (log2f(out.s) - log2_all)) * kLn2;
+      const float log_rest = __fdiv_rn(out.m - all.m, p.tau) + (logf(out.s) - log_all);
       if (rest > 0.0f) kl += rest * (logf(rest) - log_rest);
       p.loss[r] = w * (p.tau * p.tau) * kl;
-      p.stats[2ll * r] = (all.m + log2_all) * kLn2;
-      p.stats[2ll * r + 1] = (out.m + log2f(out.s)) * kLn2;
+      p.stats[2ll * r] = __fdiv_rn(all.m, p.tau) + log_all;
+      p.stats[2ll * r + 1] = __fdiv_rn(out.m, p.tau) + logf(out.s);
     }
   }
   if (!p.grad) return;
@@ -340,15 +347,18 @@ __global__ void __launch_bounds__(512, kCluster ? 1 : 2)
   const float up = (backward ? w * p.upstream[r] : w) * p.tau;
   // The student's probability of the rest as one class; of its gradient each
   // token has its part.  Where the class has no probability nothing is divided.
-  const float p_rest = out.m == -inf ? 0.0f : out.s * fast_exp2(out.m - all.m) / all.s;
+  const float p_rest = out.m == -inf ? 0.0f : out.s * share_of(out.m, all.m, c2) / all.s;
   const float coef = out.s > 0.0f || out.s != out.s ? up * (whole * p_rest - rest) / out.s : 0.0f;
-  const auto grad_of = [&](float z) { return coef * fast_exp2(fmaf(z, c2, -ref)); };
   if (a_in == a_out) {
     for_slice<4, true>(s, [&](int v, const uint4& q) {
       float z[kVec];
       Row<T>::unpack(q, z);
 #pragma unroll
-      for (int e = 0; e < kVec; ++e) z[e] = grad_of(z[e]);
+      for (int e = 0; e < kVec; e += 2) {
+        const float2 g = __fmul2_rn(make_float2(coef, coef), row_exp2_pair(z[e], z[e + 1], ref, c2));
+        z[e] = g.x;
+        z[e + 1] = g.y;
+      }
       if (v >= s.first && v < s.last) {
         __stcs(dst + v, Row<T>::pack(z));
       } else {
@@ -361,14 +371,14 @@ __global__ void __launch_bounds__(512, kCluster ? 1 : 2)
 #pragma unroll 1
     for (int i = s.lo + tid; i < s.hi; i += nt) {
       const T z = kCluster ? reinterpret_cast<const T*>(s.kept)[i - s.index(0)] : row[i];
-      grow[i] = Row<T>::from_float(grad_of(Row<T>::to_float(z)));
+      grow[i] = Row<T>::from_float(coef * share_of(Row<T>::to_float(z), ref, c2));
     }
   }
   __syncthreads();  // the record's tokens come after
 #pragma unroll 1
   for (int k = tid, j = 0; k < p.K; k += nt, ++j)
     if (speaks >> j & 1u) {
-      const float pk = fast_exp2(fmaf(rec.z[k], c2, -all.m)) / all.s;
+      const float pk = share_of(rec.z[k], all.m, c2) / all.s;
       grow[rec.at[k]] = Row<T>::from_float(up * (whole * pk - rec.q[k]));
     }
 }
