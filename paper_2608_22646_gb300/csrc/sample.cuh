@@ -805,12 +805,13 @@ __global__ void __launch_bounds__(512, kCluster ? 1 : 2)
   // (a NaN is above every floor)
   const bool listing = p.V <= kListMax || floor.key > 0;
   uint32_t pushed = 0;
-  // Where base is far below the row's largest, or no number, the sum is taken again.
-  float off = 0.0f;
-  const bool summed = looked && !__syncthreads_or(!(sum2.x + sum2.y < 1.15e18f));
-  if (summed) {
-    off = -__fmaf_rn(base, scale, -__fmul_rn(base, scale));
-  } else {
+  // Where base is far below the row's largest, or no number, or so large that the
+  // product's rounding moves the sum by more than a few binary places (a row at its
+  // type's lowest value: by 10^30 of them), the sum is taken again.
+  float off = looked ? -__fmaf_rn(base, scale, -__fmul_rn(base, scale)) : 0.0f;
+  const bool summed = looked && !__syncthreads_or(!(sum2.x + sum2.y < 1.15e18f && fabsf(off) < 8.0f));
+  if (!summed) {
+    off = 0.0f;
     base = zmax;
     sum2 = make_float2(0.0f, 0.0f);
     for_slice<4>(s, [&](int v, const uint4& q) {
