@@ -94,24 +94,28 @@ def decode_block(head, hidden, threshold=0.3, temperature=0.7, top_p=0.95, seed=
     """Tokens of a block of masked positions: ``hidden(t)`` [P, H] bf16 are the
     rows at step t.  Every step draws a token for every masked position and
     keeps those whose probability reaches the threshold, the likeliest at
-    least.  Returns (tokens [P] int32, steps)."""
-    g = torch.Generator(device="cuda")
+    least; rows without a softmax (probability NaN, their token as
+    cai_sample_rows defines it) are kept once no other is left.  So there are at
+    most P steps.  Returns (tokens [P] int32, steps)."""
+    first = hidden(0)
+    P, device = first.shape[0], first.device
+    g = torch.Generator(device=device)
     g.manual_seed(seed)
-    P = hidden(0).shape[0]
-    tokens = torch.full((P,), cai.CAI_MASK_TOKEN, dtype=torch.int32, device="cuda")
+    tokens = torch.full((P,), cai.CAI_MASK_TOKEN, dtype=torch.int32, device=device)
     steps = 0
     while bool((tokens == cai.CAI_MASK_TOKEN).any()):
         at = torch.nonzero(tokens == cai.CAI_MASK_TOKEN).flatten()
         rows = hidden(steps)[at].contiguous()
         n = rows.shape[0]
-        logits = torch.empty((n, head.V), dtype=torch.bfloat16, device="cuda")
+        logits = torch.empty((n, head.V), dtype=torch.bfloat16, device=device)
         cai.cai_mx4_logits(head, rows, logits)
-        drawn = torch.empty(n, dtype=torch.int32, device="cuda")
-        prob = torch.empty(n, dtype=torch.float32, device="cuda")
-        settings = dict(temperature=torch.full((n,), temperature, device="cuda"),
-                        top_p=torch.full((n,), top_p, device="cuda"))
-        cai.cai_sample_rows(logits, torch.rand(n, generator=g, device="cuda"), drawn, prob, **settings)
-        keep = prob >= torch.minimum(prob.max(), torch.tensor(threshold, device="cuda"))
+        drawn = torch.empty(n, dtype=torch.int32, device=device)
+        prob = torch.empty(n, dtype=torch.float32, device=device)
+        settings = dict(temperature=torch.full((n,), temperature, device=device),
+                        top_p=torch.full((n,), top_p, device=device))
+        cai.cai_sample_rows(logits, torch.rand(n, generator=g, device=device), drawn, prob, **settings)
+        score = torch.nan_to_num(prob, nan=-1.0)
+        keep = score >= score.max().clamp(max=threshold)
         tokens[at[keep]] = drawn[keep]
         steps += 1
     return tokens, steps
