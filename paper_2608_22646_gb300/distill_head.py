@@ -62,21 +62,25 @@ class DistillLoss(torch.autograd.Function):
 
 
 class Mx4Linear(torch.autograd.Function):
-    """Logits of ``rows`` from the 4-bit head of ``W``; the gradient by W passes
-    straight through the rounding."""
+    """Logits of ``rows`` from the 4-bit head of ``W``.  Gradients pass straight
+    through the rounding: by W as if it had not been rounded, by the rows with
+    the values that the codes stand for."""
 
     @staticmethod
     def forward(ctx, W, rows, head):
-        cai.cai_mx4_update(head, W.detach())
+        values = torch.empty(W.shape, dtype=torch.bfloat16, device=W.device) if ctx.needs_input_grad[1] else None
+        cai.cai_mx4_update(head, W.detach(), values)
         out = torch.empty((rows.shape[0], W.shape[0]), dtype=torch.float32, device=rows.device)
         cai.cai_mx4_logits(head, rows, out)
-        ctx.save_for_backward(rows)
+        ctx.save_for_backward(rows, values)
         return out
 
     @staticmethod
     def backward(ctx, grad):
-        (rows,) = ctx.saved_tensors
-        return grad.T @ rows.float(), None, None
+        rows, values = ctx.saved_tensors
+        by_W = grad.T @ rows.float() if ctx.needs_input_grad[0] else None
+        by_rows = (grad @ values.float()).to(rows.dtype) if ctx.needs_input_grad[1] else None
+        return by_W, by_rows, None
 
 
 def record_of(logits, K, temperature):
