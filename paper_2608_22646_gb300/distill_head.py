@@ -30,6 +30,7 @@ if ROOT not in sys.path:
     sys.path.insert(0, ROOT)
 
 import torch
+from torch.autograd.function import once_differentiable
 
 import paper_2608_22646_gb300 as cai
 
@@ -52,6 +53,7 @@ class DistillLoss(torch.autograd.Function):
         return loss
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, grad_loss):
         logits, values, index, stats = ctx.saved_tensors
         lse, temperature, weight = ctx.rest
@@ -76,6 +78,7 @@ class Mx4Linear(torch.autograd.Function):
         return out
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, grad):
         rows, values = ctx.saved_tensors
         by_W = grad.T @ rows.float() if ctx.needs_input_grad[0] else None

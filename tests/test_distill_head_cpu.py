@@ -35,3 +35,28 @@ def test_a_block_ends_whatever_its_rows_hold(monkeypatch, probs):
     without = [i for i, p in enumerate(probs) if p != p]
     for masked in kept[:-1]:  # those whose rows have no softmax are masked until the last step
         assert set(without) <= set(masked)
+
+
+def quiet(monkeypatch):
+    """The library's calls, which leave their outputs at 1."""
+    monkeypatch.setattr(cai, "cai_mx4_update", lambda head, W, values=None: None if values is None else values.fill_(1.0))
+    monkeypatch.setattr(cai, "cai_mx4_logits", lambda head, rows, out: out.fill_(1.0))
+    monkeypatch.setattr(cai, "cai_distill_loss", lambda z, tv, ti, loss, stats, **kw: (loss.fill_(1.0), stats.fill_(1.0)))
+    monkeypatch.setattr(cai, "cai_distill_backward", lambda z, tv, ti, stats, up, grad, **kw: grad.fill_(1.0))
+
+
+def test_a_second_derivative_is_refused(monkeypatch):
+    """The gradients are the library's, which autograd cannot go through: an
+    error, and not a derivative without them."""
+    quiet(monkeypatch)
+    z = torch.zeros((2, 5), requires_grad=True)
+    record = torch.zeros((2, 3)), torch.zeros((2, 3), dtype=torch.int32), None
+    up = torch.ones(2, requires_grad=True)
+    (g,) = torch.autograd.grad(distill_head.DistillLoss.apply(z, record, 1.0, None), z, up, create_graph=True)
+    with pytest.raises(RuntimeError, match="once_differentiable"):
+        (g * z).sum().backward()
+    W, rows = torch.zeros((5, 64), requires_grad=True), torch.zeros((2, 64), requires_grad=True)
+    up = torch.ones((2, 5), requires_grad=True)
+    g = torch.autograd.grad(distill_head.Mx4Linear.apply(W, rows, None), (W, rows), up, create_graph=True)
+    with pytest.raises(RuntimeError, match="once_differentiable"):
+        (g[0].sum() + g[1].sum() + (W * W).sum()).backward()
