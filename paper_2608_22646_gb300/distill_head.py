@@ -48,18 +48,17 @@ class DistillLoss(torch.autograd.Function):
         values, index, lse = record
         cai.cai_distill_loss(logits, values, index, loss, stats, top_lse=lse, temperature=temperature,
                              weight=weight)
-        ctx.save_for_backward(logits, values, index, stats)
-        ctx.rest = lse, temperature, weight
+        ctx.save_for_backward(logits, values, index, stats, lse, weight)
+        ctx.temperature = temperature
         return loss
 
     @staticmethod
     @once_differentiable
     def backward(ctx, grad_loss):
-        logits, values, index, stats = ctx.saved_tensors
-        lse, temperature, weight = ctx.rest
+        logits, values, index, stats, lse, weight = ctx.saved_tensors
         grad = torch.empty_like(logits)
         cai.cai_distill_backward(logits, values, index, stats, grad_loss.float().contiguous(), grad,
-                                 top_lse=lse, temperature=temperature, weight=weight)
+                                 top_lse=lse, temperature=ctx.temperature, weight=weight)
         return grad, None, None, None
 
 

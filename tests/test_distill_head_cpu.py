@@ -60,3 +60,18 @@ def test_a_second_derivative_is_refused(monkeypatch):
     g = torch.autograd.grad(distill_head.Mx4Linear.apply(W, rows, None), (W, rows), up, create_graph=True)
     with pytest.raises(RuntimeError, match="once_differentiable"):
         (g[0].sum() + g[1].sum() + (W * W).sum()).backward()
+
+
+@pytest.mark.parametrize("which", ["values", "index", "lse", "weight"])
+def test_a_change_in_place_between_the_calls_is_noticed(monkeypatch, which):
+    """The backward call reads the record and the weights again."""
+    quiet(monkeypatch)
+    z = torch.zeros((2, 5), requires_grad=True)
+    given = dict(values=torch.zeros((2, 3)), index=torch.zeros((2, 3), dtype=torch.int32), lse=torch.zeros(2),
+                 weight=torch.ones(2))
+    loss = distill_head.DistillLoss.apply(z, (given["values"], given["index"], given["lse"]), 1.0, given["weight"])
+    loss.sum().backward(retain_graph=True)
+    assert (z.grad == 1.0).all()
+    given[which].zero_()
+    with pytest.raises(RuntimeError, match="inplace"):
+        loss.sum().backward()
