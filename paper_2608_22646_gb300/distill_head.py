@@ -42,6 +42,8 @@ class DistillLoss(torch.autograd.Function):
 
     @staticmethod
     def forward(ctx, logits, record, temperature, weight):
+        if ctx.needs_input_grad[3]:
+            raise ValueError("weight: the loss has a gradient by the logits only")
         M = logits.shape[0]
         loss = torch.empty(M, dtype=torch.float32, device=logits.device)
         stats = torch.empty((M, 2), dtype=torch.float32, device=logits.device)

@@ -75,3 +75,11 @@ def test_a_change_in_place_between_the_calls_is_noticed(monkeypatch, which):
     given[which].zero_()
     with pytest.raises(RuntimeError, match="inplace"):
         loss.sum().backward()
+
+
+def test_what_has_no_gradient_is_refused(monkeypatch):
+    quiet(monkeypatch)
+    z = torch.zeros((2, 5), requires_grad=True)
+    record = torch.zeros((2, 3)), torch.zeros((2, 3), dtype=torch.int32), None
+    with pytest.raises(ValueError):
+        distill_head.DistillLoss.apply(z, record, 1.0, torch.ones(2, requires_grad=True))
