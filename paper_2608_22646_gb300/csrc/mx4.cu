@@ -305,14 +305,12 @@ extern "C" int cai_mx4_logits(cai_mx4* h, const void* rows, int32_t dtype, int32
     cudaGetLastError();
     return CAI_ERR_CUDA;
   }
-  p.n_mt = 1;
   p.a_rows = (M + 7) / 8 * 8;
   p.a_bytes = p.a_rows * 128;
   p.stages = kMx4MaxStages;
   while (p.stages > 2 && mx4_smem_bytes(p.stages, p.a_bytes, p.tile, elem_bytes(out_dtype)) > h->smem_limit)
     --p.stages;
-  const long long tiles = static_cast<long long>(p.n_vt) * p.n_mt;
-  const int grid = static_cast<int>(tiles < h->sms ? tiles : h->sms);
+  const int grid = p.n_vt < h->sms ? p.n_vt : h->sms;
   const size_t smem = mx4_smem_bytes(p.stages, p.a_bytes, p.tile, elem_bytes(out_dtype));
   const bool ok = out_dtype == CAI_BF16 ? launch_product<__nv_bfloat16>(p, grid, smem, s)
                                         : launch_product<float>(p, grid, smem, s);

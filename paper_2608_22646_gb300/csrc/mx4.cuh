@@ -287,7 +287,8 @@ struct Mx4Params {
   void* out;             // [M, V], ld apart
   long long ld;
   int M, V, KB, tile;
-  int n_vt, n_mt;        // tiles along V, along M
+  int n_vt;              // tiles along V
+  int n_mt;              // tiles of 256 rows along M (the pair kernel)
   int a_rows;            // rows of a row tile that are loaded (a multiple of 8)
   int a_bytes;           // room for their codes (a multiple of 1 KiB)
   int stages;
@@ -480,7 +481,7 @@ __global__ void __launch_bounds__(kMx4Threads, 1) mx4_logits_kernel(const Mx4Par
   const int sstage = mx4_smem_stage(p.a_bytes, p.tile);
   const int b_bytes = mx4_stage_bytes(p.tile);
   uint8_t* staging = smem + static_cast<size_t>(p.stages) * sstage + 16384;
-  const int tiles = p.n_vt * p.n_mt;
+  const int tiles = p.n_vt;
   if (threadIdx.x == 0) {
     for (int s = 0; s < p.stages; ++s) {
       mbar_init(&full[s], 1);
@@ -507,7 +508,7 @@ __global__ void __launch_bounds__(kMx4Threads, 1) mx4_logits_kernel(const Mx4Par
   grid_dependency_wait();
 
   if (warp == 0) {
-    const uint64_t pol_w = p.n_mt > 1 ? policy_evict_last() : policy_evict_first();
+    const uint64_t pol_w = policy_evict_first();
     const uint64_t pol_r = policy_evict_last();
     const bool leader = elect_one();
     const int a_codes = p.a_rows * 128;
@@ -516,9 +517,7 @@ __global__ void __launch_bounds__(kMx4Threads, 1) mx4_logits_kernel(const Mx4Par
     int issued = 0;
     bool ok = true;
     for (int t = blockIdx.x; t < tiles && ok; t += gridDim.x) {
-      const int vt = t / p.n_mt, mt = t - vt * p.n_mt;
-      const uint8_t* wsrc = p.w + static_cast<size_t>(vt) * p.KB * b_bytes;
-      const uint8_t* rsrc = p.rows + static_cast<size_t>(mt) * p.KB * kRowStage;
+      const uint8_t* wsrc = p.w + static_cast<size_t>(t) * p.KB * b_bytes;
       for (int kb = 0; kb < p.KB; ++kb) {
         ok = ok && mbar_wait(&empty[r.slot], r.phase ^ 1u, &abort_flag, p.err, kErrWaitEmpty);
         if (leader && ok) {
@@ -526,7 +525,7 @@ __global__ void __launch_bounds__(kMx4Threads, 1) mx4_logits_kernel(const Mx4Par
           mbar_arrive_expect_tx(&full[r.slot], b_bytes + a_codes + mx4_scale_bytes(kMx4RowTile));
           bulk_load(s + p.a_bytes + mx4_scale_bytes(kMx4RowTile), wsrc + static_cast<size_t>(kb) * b_bytes,
                     b_bytes, &full[r.slot], pol_w);
-          const uint8_t* a = rsrc + static_cast<size_t>(kb) * kRowStage;
+          const uint8_t* a = p.rows + static_cast<size_t>(kb) * kRowStage;
           bulk_load(s, a, a_codes, &full[r.slot], pol_r);
           bulk_load(s + p.a_bytes, a + kMx4RowTile * 128, mx4_scale_bytes(kMx4RowTile), &full[r.slot], pol_r);
         }
@@ -559,9 +558,7 @@ __global__ void __launch_bounds__(kMx4Threads, 1) mx4_logits_kernel(const Mx4Par
     for (int t = blockIdx.x; t < tiles; t += gridDim.x) {
       if (!mbar_wait(&accf[acc.slot], acc.phase, &abort_flag, p.err, kErrWaitAccFull)) break;
       tc_fence_after();
-      const int vt = t / p.n_mt, mt = t - vt * p.n_mt;
-      const int row0 = mt * kMx4RowTile + quarter * 32;
-      const int v0 = vt * p.tile;
+      const int row0 = quarter * 32, v0 = t * p.tile;
       mx4_store_tile<T>(tmem + acc.slot * kMx4AccCol + (static_cast<uint32_t>(quarter * 32) << 16), mine,
                         static_cast<T*>(p.out) + static_cast<long long>(row0) * p.ld + v0, p.ld,
                         p.M - row0, min(p.tile, p.V - v0), aligned, part);
