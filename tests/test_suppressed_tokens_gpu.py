@@ -115,3 +115,24 @@ def test_suppressed_tokens(M, dtype, tau, tail):
     g = torch.full((M, V), 99.0, dtype=dtype, device="cuda")
     cai.cai_distill_backward(z, tv, ti, stats, up, g, top_lse=tlse, temperature=tau, weight=w)
     check(z, tv, ti, tlse, tau, w, None, None, g, some, up)
+
+
+@pytest.mark.parametrize("M", [8, 200])
+@pytest.mark.parametrize("tail", [False, True])
+def test_students_without_a_softmax(M, tail):
+    """A NaN or +inf, in the record or not, and rows with nothing above -inf: the
+    loss is NaN, and no other row's."""
+    inf = float("inf")
+    for dtype in (BF16, F32):
+        z = rows_of(M, V, dtype, 12)
+        ti = torch.arange(K, dtype=torch.int32, device="cuda").mul(3).expand(M, K).contiguous()
+        tv = torch.randn((M, K), generator=torch.Generator().manual_seed(4)).cuda()
+        tlse = torch.logsumexp(tv, 1) + 0.4 if tail else None
+        z[0, 40000] = float("nan")
+        z[1, 3] = float("nan")
+        z[2, 40000] = inf
+        z[3, 3] = inf
+        z[4] = -inf
+        loss, stats, grad = loss_of(z, tv, ti, tlse, 1.0, None)
+        assert torch.isnan(loss[:5]).all() and torch.isfinite(loss[5:]).all()
+        assert torch.isfinite(stats[5:]).all() and torch.isfinite(grad[5:].float()).all()
