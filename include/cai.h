@@ -458,7 +458,8 @@ int cai_test_static_wait_timeout(void);
  * Draws one token from every row.  temperature, top_k, top_p, min_p: device
  * arrays of M entries, or NULL for 1, off, off, off; u: M uniform numbers in
  * [0, 1) (others are clamped into it, NaN is 0).  Per row, with T its temperature:
- *   e_i = 2^((z_i - max z) (log2(e) / T)) in fp32, each operation rounded once,
+ *   e_i = 2^((z_i - max z) (log2(e) / T)) in fp32: quotient, difference and
+ *   product rounded once each, the power good to 2 ulp;
  *   w_i = e_i in units of 2^-40, rounded to the nearest whole number;
  *   tokens are ordered by falling z, ties by rising index (-0 equals +0);
  *   top_k in [1, V) keeps the first top_k tokens (else off), min_p keeps those
@@ -500,8 +501,11 @@ int cai_top_rows(const void* logits, int32_t dtype, int64_t ld, int32_t M, int32
  * and over the tokens outside the record, for the backward call.  A row with
  * weight 0, or without entries, is not read: loss, stats and gradient 0.
  * grad (NULL: none): dloss/dz of every row, [M, V] of `dtype`, ld_grad apart;
- * it may be the logits' own buffer with ld_grad = ld.  Where no token outside
- * the record has any probability, those tokens' gradient is that of p alone.
+ * it may be the logits' own buffer with ld_grad = ld.  Finite logits may be of
+ * any size, the type's lowest value among them; where the result passes what
+ * fp32 holds, a loss is +inf.  Where every token outside the record is at -inf,
+ * those tokens' gradient is that of p alone.  A row without a softmax (a NaN or
+ * +inf logit, or none above -inf) has loss NaN and no gradient of use.
  */
 int cai_distill_loss(const void* logits, int32_t dtype, int64_t ld, int32_t M, int32_t V,
                      int32_t K, const float* top_values, const int32_t* top_index,

@@ -66,8 +66,8 @@ class DistillLoss(torch.autograd.Function):
 
 class Mx4Linear(torch.autograd.Function):
     """Logits of ``rows`` from the 4-bit head of ``W``.  Gradients pass straight
-    through the rounding: by W as if it had not been rounded, by the rows with
-    the values that the codes stand for."""
+    through the rounding: by W it is the gradient times the rows as given, by
+    the rows the gradient times the values that W's codes stand for."""
 
     @staticmethod
     def forward(ctx, W, rows, head):
