@@ -714,8 +714,11 @@ int cai_norm_backward(const void* x, int32_t dtype, int64_t ld, const void* grad
  * with the probability of their distance, by 16 bits each of a hash of (seed, t,
  * the tensor's place in the table, the element's place in the tensor): rounding
  * to nearest would hold a v that changes by a thousandth a step where it is.
- * Numbers that are not 0 keep a code that is not 0.  A block with a NaN or an
- * infinity has power 255: it stands for NaNs.
+ * Numbers that are not 0 keep a code that is not 0, but for an m whose share of the
+ * gradient, |(1 - beta1) g|, is below the block's smallest number, 2^(power - 9), where
+ * the element's root was not 0 before the step: it may become 0, so that what has no
+ * gradient any more comes to rest.  A block with a NaN or an infinity has power 255: it
+ * stands for NaNs.
  *   hash: k = mix(mix(mix(mix(seed) + t) + place) + element / 2^32),
  *   h = mix(k + 0x9e3779b1 element), all mod 2^32; mix(x): x ^= x >> 16,
  *   x *= 0x7feb352d, x ^= x >> 15, x *= 0x846ca68b, x ^= x >> 16; m takes the low

@@ -7,7 +7,10 @@
 // beta2 = 0.999 a v moves by a thousandth of itself a step, E4M3's step is an eighth:
 // rounded to nearest it would never move.  So the last place is rounded up with
 // the probability of what is cut off; where that makes 0 of a number, 1 is kept,
-// since a root of 0 under an m that is not would divide by eps.
+// since a root of 0 under an m that is not would divide by eps.  But an m that its
+// gradient does not bring to the smallest code may become 0 once it has a root: kept at
+// 1 it would hold its sign for as long as its block has larger numbers, while its root
+// decays, and in time move a parameter whose gradient has ended by some lr a step.
 #pragma once
 
 #include <cuda_bf16.h>
@@ -73,14 +76,20 @@ __device__ __forceinline__ int power_for(uint32_t top) {
   const int b = static_cast<int>(top >> 23) - 8 + ((top & 0x7fffffu) > 0x600000u ? 1 : 0);
   return b < 0 ? 0 : b;
 }
-// x under the biased power `byte`, rounded up where 16 bits of dither carry.
-__device__ __forceinline__ uint32_t e4m3_code(float x, int byte, uint32_t dither) {
+// x under the biased power `byte`, rounded up where 16 bits of dither carry; `least`:
+// what a number that is not 0 has at least.
+__device__ __forceinline__ uint32_t e4m3_code(float x, int byte, uint32_t dither, uint32_t least) {
   const float y = __fmul_rn(fabsf(x), __uint_as_float(static_cast<uint32_t>(254 - (byte < 254 ? byte : 0)) << 23));
   // E4M3's exponent and mantissa are those of y 2^-120 in fp32, denormals too.
   uint32_t code = (__float_as_uint(__fmul_rn(y, 0x1p-120f)) + (dither << 4)) >> 20;
   if (byte == 255) return 0;
-  if (x != 0.0f && code == 0) code = 1;
-  return code | (__float_as_uint(x) >> 24 & (x != 0.0f ? 0x80u : 0u));
+  if (x != 0.0f && code == 0) code = least;
+  return code | (__float_as_uint(x) >> 24 & (code != 0 ? 0x80u : 0u));
+}
+// Whether m's share of its gradient, (1 - beta1) g, is below the smallest number under
+// the biased power `byte`.
+__device__ __forceinline__ bool e4m3_below(float share, int byte) {
+  return __fmul_rn(fabsf(share), __uint_as_float(static_cast<uint32_t>(254 - byte) << 23)) < 0x1p-9f;
 }
 
 // Two sums, each rounded once.  The compiler makes one operation of a packed product
@@ -199,7 +208,9 @@ __device__ __forceinline__ float magnitude(const float (&x)[8]) {  // NaN kept
 }
 
 // The E4M3 codes of eight elements' m and root under their blocks' biased powers; k:
-// the first one's hash before its mixing.
+// the first one's hash before its mixing.  An m that is not 0 may have the code 0: see
+// settled_m.  (Its sign is set under a comparison: nvcc 13.0.88 puts a sign that is
+// always set together with a wrong byte of the fourth code.)
 __device__ __forceinline__ void e4m3_codes8(const float (&m)[8], int bm, const float (&root)[8], int bv, uint32_t k,
                                             uint2& cm, uint2& cv) {
   const float dm = __uint_as_float(static_cast<uint32_t>(254 - (bm < 254 ? bm : 0)) << 23);
@@ -213,7 +224,7 @@ __device__ __forceinline__ void e4m3_codes8(const float (&m)[8], int bm, const f
                                 make_float2(0x1p-120f, 0x1p-120f));
     uint32_t c = (__float_as_uint(y.x) + (h << 16 >> 12)) >> 20;
     uint32_t d = (__float_as_uint(y.y) + (h >> 16 << 4)) >> 20;
-    if (m[e] != 0.0f) c = max(c, 1u) | (__float_as_uint(m[e]) >> 24 & 0x80u);
+    if (m[e] != 0.0f) c |= __float_as_uint(m[e]) >> 24 & 0x80u;
     if (root[e] != 0.0f) d = max(d, 1u);
     wm[e / 4] |= c << (8 * (e & 3));
     wv[e / 4] |= d << (8 * (e & 3));
@@ -221,6 +232,9 @@ __device__ __forceinline__ void e4m3_codes8(const float (&m)[8], int bm, const f
   cm = bm == 255 ? make_uint2(0u, 0u) : make_uint2(wm[0], wm[1]);
   cv = bv == 255 ? make_uint2(0u, 0u) : make_uint2(wv[0], wv[1]);
 }
+
+// The bytes of w that are 0 but for their highest bit: that bit of theirs.
+__device__ __forceinline__ uint32_t no_code(uint32_t w) { return ~((w & 0x7f7f7f7fu) + 0x7f7f7f7fu) & 0x80808080u; }
 
 // One tensor's elements [from, to), from a multiple of the chunk, to its end or
 // another.
@@ -258,6 +272,31 @@ struct AdamRun {
       v.load(static_cast<const float*>(a.v) + j);
     }
   };
+
+  // Eight codes of m, those of 0 (`none`: their bytes' highest bits) made final: 1 for a
+  // number that keeps a code (`some`: a bit for every m that is not 0), else 0.  Rare, so
+  // what it needs is read again: the gradients, and the roots' codes before the new ones
+  // are written.
+  template <typename G>
+  __device__ __noinline__ uint64_t settled_m(uint64_t codes, uint64_t none, unsigned some, int power, const G* grad,
+                                             const uint8_t* root) const {
+#pragma unroll 1
+    for (; none != 0; none &= none - 1) {
+      const int bit = __ffsll(static_cast<long long>(none)) - 1, e = bit >> 3;
+      const bool keeps =
+          (some >> e & 1u) && (root[e] == 0 || !e4m3_below(__fmul_rn(gradient(grad, e), s.c1), power));
+      if (keeps)
+        codes |= 1ull << (bit - 7);
+      else
+        codes &= ~(1ull << bit);
+    }
+    return codes;
+  }
+  template <typename G>
+  __device__ __forceinline__ float gradient(const G* grad, long long i) const {
+    const float g = Row<G>::to_float(grad[i]);
+    return s.scaled ? __fmul_rn(g, s.scale) : g;
+  }
 
   // Eight elements to a thread, blocks of 32 to four lanes; with 8-bit states the
   // next eight are on their way meanwhile.  At most 2^30 elements.
@@ -303,6 +342,17 @@ struct AdamRun {
         const long long i = from + j;
         uint2 cm, cv;
         e4m3_codes8(m, bm, root, bv, key_at(i) + 0x9e3779b1u * static_cast<uint32_t>(i), cm, cv);
+        const uint2 none = make_uint2(no_code(cm.x), no_code(cm.y));
+        if ((none.x | none.y) != 0u && bm != 255) {
+          unsigned some = 0;  // the m that are not 0
+#pragma unroll
+          for (int e = 0; e < 8; ++e) some |= (m[e] != 0.0f ? 1u : 0u) << e;
+          const uint64_t codes = some ? settled_m(static_cast<uint64_t>(cm.y) << 32 | cm.x,
+                                                  static_cast<uint64_t>(none.y) << 32 | none.x, some, bm, grad + j,
+                                                  static_cast<const uint8_t*>(a.v) + j)
+                                      : 0;
+          cm = make_uint2(static_cast<uint32_t>(codes), static_cast<uint32_t>(codes >> 32));
+        }
         __stcs(reinterpret_cast<uint2*>(static_cast<uint8_t*>(a.m) + j), cm);
         __stcs(reinterpret_cast<uint2*>(static_cast<uint8_t*>(a.v) + j), cv);
         if ((lane & 3) == 0) {
@@ -322,6 +372,7 @@ struct AdamRun {
       const long long i = b + lane;
       const bool in = i < to;
       float p[2] = {}, g[2] = {}, m[2] = {}, v[2] = {}, root[2] = {};
+      bool had_root = false;
       if (in) {
         g[0] = grad_bf16 ? __bfloat162float(static_cast<const __nv_bfloat16*>(grad)[i]) : static_cast<const float*>(grad)[i];
         p[0] = a.bf16 ? __bfloat162float(static_cast<const __nv_bfloat16*>(a.param)[i]) : static_cast<const float*>(a.param)[i];
@@ -331,6 +382,7 @@ struct AdamRun {
         } else {
           m[0] = __fmul_rn(e4m3_value(static_cast<const uint8_t*>(a.m)[i]), power_of(a.m_scale[i >> 5]));
           root[0] = __fmul_rn(e4m3_value(static_cast<const uint8_t*>(a.v)[i]), power_of(a.v_scale[i >> 5]));
+          had_root = static_cast<const uint8_t*>(a.v)[i] != 0;
         }
         adam_update<kBits>(s, p, g, m, v, root);
         if (a.bf16)
@@ -350,8 +402,10 @@ struct AdamRun {
         const int bm = power_for(__reduce_max_sync(0xffffffffu, __float_as_uint(m[0]) & 0x7fffffffu));
         const int bv = power_for(__reduce_max_sync(0xffffffffu, __float_as_uint(root[0]) & 0x7fffffffu));
         if (in) {
-          static_cast<uint8_t*>(a.m)[i] = static_cast<uint8_t>(e4m3_code(m[0], bm, h & 0xffffu));
-          static_cast<uint8_t*>(a.v)[i] = static_cast<uint8_t>(e4m3_code(root[0], bv, h >> 16));
+          const float share = __fmul_rn(s.scaled ? __fmul_rn(g[0], s.scale) : g[0], s.c1);
+          const bool ends = bm != 255 && had_root && e4m3_below(share, bm);
+          static_cast<uint8_t*>(a.m)[i] = static_cast<uint8_t>(e4m3_code(m[0], bm, h & 0xffffu, ends ? 0u : 1u));
+          static_cast<uint8_t*>(a.v)[i] = static_cast<uint8_t>(e4m3_code(root[0], bv, h >> 16, 1u));
         }
         if (lane == 0) {
           a.m_scale[i >> 5] = static_cast<uint8_t>(bm);
