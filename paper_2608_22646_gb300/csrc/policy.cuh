@@ -805,9 +805,10 @@ __global__ void __launch_bounds__(kPairThreads) preference_kernel(const __grid_c
   const float e = expf(-fabsf(margin));              // in (0, 1]
   const float down = (margin >= 0.0f ? e : 1.0f) / (1.0f + e);  // sigmoid(-margin)
   if (tid == 0) {
-    // -log sigmoid(x) = log(1 + exp(-|x|)) + max(-x, 0)
-    const float smooth = p.smoothing != 0.0f ? p.smoothing * margin : 0.0f;
-    p.loss[i] = margin != margin ? margin : log1pf(e) + fmaxf(-margin, 0.0f) + smooth;
+    // -log sigmoid(x) = log(1 + exp(-|x|)) + max(-x, 0): of the two terms one has the |x|.  (A
+    // margin is infinite where a token is suppressed; a share of 0 has no term.)
+    const float share = margin < 0.0f ? 1.0f - p.smoothing : p.smoothing;
+    p.loss[i] = margin != margin ? margin : log1pf(e) + (share != 0.0f ? share * fabsf(margin) : 0.0f);
     p.margin[i] = margin;
   }
   if (!p.grad_logp) return;
