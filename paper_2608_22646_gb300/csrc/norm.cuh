@@ -420,7 +420,6 @@ __global__ void __launch_bounds__(kThreads, 1)
   const int at = threadIdx.x % span, unit = threadIdx.x / span, warp = at / 32;
   const int slots = (warps + 3) & ~3, first = unit * slots;
   const long long step = static_cast<long long>(gridDim.x) * units;
-  const float inv_h = __fdiv_rn(1.0f, p.H);
   const int lowest = at / 32 * (32 * kElems) + lane * kN;
   const auto col = [&](int k) { return lowest + k * 32 * kN; };
   const long long row0 = static_cast<long long>(unit) * gridDim.x + blockIdx.x;
@@ -498,7 +497,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       }
     }
     ask();
-    const float mean = p.layer ? row_sum(whole(sum)) * inv_h : 0.0f;
+    const float mean = p.layer ? __fdiv_rn(row_sum(whole(sum)), p.H) : 0.0f;
     const P off = splat<P>(-mean);
     sum = splat<P>(0.0f);
 #pragma unroll
