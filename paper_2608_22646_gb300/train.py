@@ -188,15 +188,20 @@ class AdamW:
     @torch.no_grad()
     def step(self, grad_scale=None, lr_step=None) -> None:
         """A step of every parameter with a gradient.  ``grad_scale`` and
-        ``lr_step``: see cai_adamw_step."""
-        for params, places, _ in self.groups:
-            for p, at in zip(params, places):
-                if p.data_ptr() != at:
+        ``lr_step``: see cai_adamw_step.  ``steps`` counts the calls that succeeded: a
+        step that is refused is none, and moves no parameter.  (A captured one is counted
+        once: who replays it with ``lr_step`` sets ``steps`` to its t before a
+        state_dict().)"""
+        # What one group alone could be refused for, before any group moves; settings
+        # are the same for all, and looked at by the first one's call.
+        step, work = self.steps + 1, []
+        for params, places, opt in self.groups:
+            for p, at, t in zip(params, places, opt.tensors):
+                if p.data_ptr() != at or p.numel() != t["param"].numel():
                     raise RuntimeError("AdamW: a parameter has another storage than when the optimiser was made")
-        self.steps += 1
-        for params, _, opt in self.groups:
-            grads = [None if p.grad is None else p.grad.to(p.dtype).contiguous() for p in params]
-            cai.cai_adamw_step(opt, grads, lr=self.lr, step=self.steps, beta1=self.betas[0], beta2=self.betas[1],
+            work.append([None if p.grad is None else p.grad.to(p.dtype).contiguous() for p in params])
+        for (params, _, opt), grads in zip(self.groups, work):
+            cai.cai_adamw_step(opt, grads, lr=self.lr, step=step, beta1=self.betas[0], beta2=self.betas[1],
                                eps=self.eps, seed=self.seed, grad_scale=grad_scale, lr_step=lr_step)
             # What autograd has kept of them is not what they are any more.
             for p, g, t in zip(params, grads, opt.tensors):
@@ -204,6 +209,7 @@ class AdamW:
                     torch.autograd.graph.increment_version(p)
                     if t["copy"] is not None:
                         torch.autograd.graph.increment_version(t["copy"])
+        self.steps = step
 
     def state_dict(self) -> dict:
         return dict(steps=self.steps, seed=self.seed, state_bits=self.state_bits,
