@@ -156,7 +156,7 @@ class AdamW:
     """AdamW over ``params`` (contiguous CUDA parameters, float32 or bf16) with
     one launch a step for every kind of them.  ``state_bits`` 8 keeps the states
     as E4M3 in blocks of 32, a quarter of their bytes, rounded by a hash of
-    ``seed``, the step and the element.  ``copies``: {parameter: bf16 tensor} of
+    ``seed``, the parameter's type and place, the step and the element.  ``copies``: {parameter: bf16 tensor} of
     float32 parameters whose rounded values are written along.  ``decay`` may be
     a function of a parameter."""
 
@@ -200,9 +200,12 @@ class AdamW:
                 if p.data_ptr() != at or p.numel() != t["param"].numel():
                     raise RuntimeError("AdamW: a parameter has another storage than when the optimiser was made")
             work.append([None if p.grad is None else p.grad.to(p.dtype).contiguous() for p in params])
-        for (params, _, opt), grads in zip(self.groups, work):
+        for i, ((params, _, opt), grads) in enumerate(zip(self.groups, work)):
+            # A group counts its tensors from 0: another seed, or the first of each would be
+            # rounded alike.  (From the group's number alone, so that a loaded state goes on.)
+            seed = (self.seed + 0x9e3779b9 * i) & 0xffffffff
             cai.cai_adamw_step(opt, grads, lr=self.lr, step=step, beta1=self.betas[0], beta2=self.betas[1],
-                               eps=self.eps, seed=self.seed, grad_scale=grad_scale, lr_step=lr_step)
+                               eps=self.eps, seed=seed, grad_scale=grad_scale, lr_step=lr_step)
             # What autograd has kept of them is not what they are any more.
             for p, g, t in zip(params, grads, opt.tensors):
                 if g is not None:
