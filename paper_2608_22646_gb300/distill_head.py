@@ -24,6 +24,7 @@ before and after, and the decoded block's steps.
 from __future__ import annotations
 
 import argparse
+import contextlib
 import json
 import os
 import sys
@@ -155,10 +156,6 @@ def main(argv=None) -> int:
     student = torch.nn.Parameter(W.float())
     gain = torch.nn.Parameter(torch.ones(wl.H, device="cuda"))
     trained = [student] if args.norm == "none" else [student, gain]
-    if args.optimiser == "torch":
-        optimiser = torch.optim.Adam(trained, lr=args.lr)
-    else:
-        optimiser = train.AdamW(trained, lr=args.lr, decay=0.0, state_bits=8 if args.optimiser == "adamw8" else 32)
     held = rows(0)
 
     def normed(x):
@@ -169,7 +166,12 @@ def main(argv=None) -> int:
         # Hidden states keep the scale that the head's weight is for.
         return y * x.float().square().mean().sqrt().to(x.dtype)
 
-    with cai.cai_mx4_init(student.detach(), held.shape[0]) as head:
+    with cai.cai_mx4_init(student.detach(), held.shape[0]) as head, contextlib.ExitStack() as handles:
+        if args.optimiser == "torch":
+            optimiser = torch.optim.Adam(trained, lr=args.lr)
+        else:
+            bits = 8 if args.optimiser == "adamw8" else 32
+            optimiser = handles.enter_context(train.AdamW(trained, lr=args.lr, decay=0.0, state_bits=bits))
 
         def evaluate():
             teacher = (held @ W.T).float()

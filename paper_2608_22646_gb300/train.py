@@ -158,7 +158,9 @@ class AdamW:
     as E4M3 in blocks of 32, a quarter of their bytes, rounded by a hash of
     ``seed``, the parameter's type and place, the step and the element.  ``copies``: {parameter: bf16 tensor} of
     float32 parameters whose rounded values are written along.  ``decay`` may be
-    a function of a parameter."""
+    a function of a parameter.  Its handles live until ``close()`` or the end of a
+    ``with``: freeing them synchronises the device, which an object that is dropped
+    may not do at any time."""
 
     def __init__(self, params, lr=1e-3, betas=(0.9, 0.999), eps=1e-8, decay=0.01, state_bits=32, copies=None, seed=0):
         self.params = list({id(p): p for p in params}.values())  # shared ones once
@@ -179,7 +181,12 @@ class AdamW:
         self.groups = []  # of one dtype: gradients are all alike in a call
         for members in kinds.values():
             group = [p for p, _ in members]
-            self.groups.append((group, [p.data_ptr() for p in group], cai.cai_adamw_init([t for _, t in members], state_bits)))
+            try:
+                opt = cai.cai_adamw_init([t for _, t in members], state_bits)
+            except Exception:
+                self.close()  # the groups before
+                raise
+            self.groups.append((group, [p.data_ptr() for p in group], opt))
 
     def zero_grad(self) -> None:
         for p in self.params:
