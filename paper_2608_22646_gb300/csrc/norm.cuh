@@ -531,9 +531,10 @@ __global__ void __launch_bounds__(kThreads, 1)
   }
 }
 
-// The backward call's plan, from H alone: elements of a thread and threads of a
-// unit, which takes rows in turn and adds up its own partial sums; units of a warp
-// share CTAs of eight.
+// The backward call's plan, from H and M and never from the device: elements of a thread
+// and threads of a unit (of H alone), which takes rows in turn and adds up its own
+// partial sums; and the parts that the workspace has room for, one to a row and at most
+// norm_share to an SM.  Units of a warp share CTAs of eight.
 struct NormPlan {
   int elems, threads, parts;
 };

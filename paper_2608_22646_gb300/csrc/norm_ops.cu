@@ -156,7 +156,8 @@ bool grad_ring(const NormParams& p, int dev, cudaStream_t s) {
   const int threads = units * span, row = kNormRingThreads * kElems * 2 * static_cast<int>(sizeof(T));
   const int staged = kElems <= 16 ? 0 : staged_cols(p.H + kMore) * static_cast<int>(sizeof(float));
   const int ring = units ? std::min(8, (kMostShared - staged) / row) : 0;
-  if (ring < 2 || p.M < kNormSms || !open_shared<norm_grad_ring_kernel<T, W, kElems, kEdges>>(dev, kMostShared)) return false;
+  // (it leaves a part of every SM's: no fewer may have room)
+  if (ring < 2 || p.parts < kNormSms || !open_shared<norm_grad_ring_kernel<T, W, kElems, kEdges>>(dev, kMostShared)) return false;
   const int smem = std::max(ring * row + staged, units * 2 * p.H * static_cast<int>(sizeof(float)));
   norm_grad_ring_kernel<T, W, kElems, kEdges><<<kNormSms, threads, smem, s>>>(p, span, ring);
   return true;
@@ -182,7 +183,7 @@ bool backward(NormParams& p, int dev, cudaStream_t s) {
   const bool edges = !kWide && p.H >= 64 && (sizeof(T) == 2 || p.M >= 32 * kNormSms) && alike(p.x, p.ld, p.gy, p.ld_gy, sizeof(T)) &&
                      (!p.out || alike(p.x, p.ld, p.out, p.ld_out, sizeof(T)));
   if ((kWide || edges) && grad_rings<T, W, !kWide>(p, dev, s)) {
-    p.parts = kNormSms;
+    p.parts = kNormSms;  // of p.parts, which is parts_of(M, H) and the workspace's: as many or more
     return cudaGetLastError() == cudaSuccess;
   }
   const NormPlan plan = norm_plan(p.M, p.H);
