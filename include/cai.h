@@ -576,7 +576,10 @@ void cai_mx4_free(cai_mx4* head);
  * token t, T the temperature; stats [M, 2]: the row's largest logit and the sum of
  * exp((z_v - max) / T), for the backward call.  A token at -inf in a row with a
  * softmax has logp -inf.  A row without a softmax (a NaN or +inf logit, or none
- * above -inf) has logp NaN.
+ * above -inf) has logp NaN.  (CTAs that share a row wait for each other for 2 s at
+ * most, which no run but one that was stopped in between comes near.  There is no error
+ * word: what did not come in time, and every row that was to follow it on the same CTAs,
+ * is NaN, in what is written for the row and in its gradient.)
  * cai_token_logp_backward: grad [M, V] of `dtype`, ld_grad apart, is
  * grad_logp [M] times d logp / d z_v = ([v = t] - exp(z_v / T) / sum) / T, from the
  * stats of the same logits and temperature.  A row whose grad_logp is 0 is not
@@ -621,6 +624,17 @@ int cai_policy_backward(const void* logits, int32_t dtype, int64_t ld, int32_t M
                         const int32_t* token, double temperature, const float* stats,
                         const float* slope, const float* grad_loss, void* grad, int64_t ld_grad,
                         void* stream);
+
+/*
+ * Testing hook: cai_policy_loss of dense float32 rows at temperature 1 (without old_logp,
+ * ref_logp and weight; grad NULL: none) by one cluster of `ctas` (2, 4 or 8) CTAs, of
+ * which one waits 0.6 s before it tells the others its sums of row late_row, while they
+ * wait for 0.2 s.  Rows from late_row on that take part are NaN.  No trap and no fault.  1024 ctas <= V <= 4096 ctas,
+ * V a multiple of 4, rows on 16-byte boundaries, 0 <= late_row < M.
+ */
+int cai_test_late_rows(const float* logits, int32_t M, int32_t V, const int32_t* token,
+                       const float* advantage, int32_t ctas, int32_t late_row, float* loss,
+                       float* logp, float* stats, float* slope, float* grad, void* stream);
 
 /*
  * The preference loss of pairs of sequences, from their tokens' log-probabilities

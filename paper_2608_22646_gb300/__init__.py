@@ -64,7 +64,7 @@ EXPORTS = ("cai_config_default", "cai_init", "cai_init_rmsnorm", "cai_first_step
            "cai_sample_rows", "cai_top_rows", "cai_distill_loss", "cai_distill_backward",
            "cai_mx4_init", "cai_mx4_update", "cai_mx4_logits", "cai_mx4_error_bits", "cai_mx4_free",
            "cai_token_logp", "cai_token_logp_backward", "cai_policy_loss", "cai_policy_backward",
-           "cai_preference_loss", "cai_norm_rows", "cai_norm_workspace", "cai_norm_backward",
+           "cai_test_late_rows", "cai_preference_loss", "cai_norm_rows", "cai_norm_workspace", "cai_norm_backward",
            "cai_adamw_init", "cai_adamw_step", "cai_adamw_free")
 
 
@@ -169,6 +169,7 @@ def _load():
         "cai_policy_loss": (ctypes.c_int, [vp, i32, i64, i32, i32, vp, vp, vp, vp, vp, f64, f64, f64, f64,
                                            vp, vp, vp, vp, vp, i64, vp]),
         "cai_policy_backward": (ctypes.c_int, [vp, i32, i64, i32, i32, vp, f64, vp, vp, vp, vp, i64, vp]),
+        "cai_test_late_rows": (ctypes.c_int, [vp, i32, i32, vp, vp, i32, i32, vp, vp, vp, vp, vp, vp]),
         "cai_preference_loss": (ctypes.c_int, [vp, vp, vp, vp, i32, i32, f64, f64, vp, vp, vp, vp, vp]),
         "cai_norm_rows": (ctypes.c_int, [vp, i32, i64, i32, i32, i32, vp, vp, i32, f64, vp, i64, vp, vp]),
         "cai_norm_workspace": (ctypes.c_int, [i32, i32, ctypes.POINTER(i64)]),
@@ -767,6 +768,19 @@ def cai_policy_backward(logits, token, stats, slope, grad_loss, grad, temperatur
     by, up = _vectors(M, "float32", "slope", slope, "grad_loss", grad_loss)
     _check(lib().cai_policy_backward(ptr, code, ld, M, V, t, temperature, _arr(stats, "stats", "float32", (M, 2)), by, up,
                                      gptr, gld, _stream(stream)), "cai_policy_backward")
+
+
+def cai_test_late_rows(logits, token, advantage, loss, logp, stats, slope, grad=None, ctas: int = 4,
+                       late_row: int = 0, stream=None) -> None:
+    """cai_policy_loss of float32 ``logits`` by one cluster, of which a CTA comes
+    late with its sums of ``late_row``: rows from there on are NaN."""
+    M, V = logits.shape
+    (t,) = _vectors(M, "int32", "token", token)
+    adv, out, lp, by = _vectors(M, "float32", "advantage", advantage, "loss", loss, "logp", logp, "slope", slope)
+    _check(lib().cai_test_late_rows(_arr(logits, "logits", "float32", (M, V)), M, V, t, adv, ctas, late_row, out, lp,
+                                    _arr(stats, "stats", "float32", (M, 2)), by,
+                                    None if grad is None else _arr(grad, "grad", "float32", (M, V)), _stream(stream)),
+           "cai_test_late_rows")
 
 
 def cai_preference_loss(logp, offsets, loss, margin, grad_logp=None, ref_logp=None, weight=None,

@@ -164,6 +164,7 @@ struct TokenPlan {
   int batches;  // of a row
   int ring;     // batches; with the gradient, more than a row's; under three rows'
   int clusters;
+  int late_turn;  // (a test's form alone: before its sums of this turn a CTA waits past the others' limit)
 };
 
 // How rows lie: whole vectors of 16 bytes; anywhere, logits and gradient alike; the gradient
@@ -176,12 +177,19 @@ constexpr int kBatch = 4;
 // What the CTAs of a cluster tell each other of a row, in turn in one of two places: a
 // row's is written again for the next but one, which takes every warp's sum of the
 // next, which it gives when it has read this one's.
+//
+// A warp whose wait runs out is deaf from there on: it tells nothing more, since it would
+// write over what others have not read, and says so to every CTA of the cluster.  Nobody
+// can then hear of a later row: who waits becomes deaf as it learns of it, or in its own
+// time.  A deaf warp's rows are NaN, loss, stats and gradient, from the row on that it did
+// not hear of; a number that was written came from all sums of its row.
 struct TokenShared {
   float4 part[2][kRowMaxCluster * kTokenMaxWarps];  // a warp's sum, of every CTA of the cluster
   TokenRow info[2];
   float zt[2];         // the token's logit, from the CTA that has it
   uint64_t full[2];    // counts the bytes of the above
   TokenRow row[4];     // copied with a row's first batch, each field by a thread that gives it on
+  unsigned deaf;       // a warp of the cluster is
 };
 
 // Writes 4 or 16 bytes into the same place of another CTA's shared memory and counts them at its
@@ -198,14 +206,26 @@ __device__ __forceinline__ void tell(float4* dst, uint64_t* bar, int rank, const
                "r"(mapa_shared(bar, rank))
                : "memory");
 }
-// Waits for a phase; false after kWaitLimitNs.
-__device__ __forceinline__ bool heard(uint64_t* bar, uint32_t parity) {
+__device__ __forceinline__ void tell_deaf(unsigned* flag, int rank) {
+  asm volatile("st.relaxed.cluster.shared::cluster.u32 [%0], 1;" ::"r"(mapa_shared(flag, rank)) : "memory");
+}
+__device__ __forceinline__ bool any_deaf(const unsigned* flag) {
+  uint32_t x;
+  asm volatile("ld.relaxed.cluster.shared::cta.u32 %0, [%1];" : "=r"(x) : "r"(smem_addr(flag)) : "memory");
+  return x != 0;
+}
+// Waits for a phase; false after `limit` ns, or where a warp of the cluster is deaf.
+__device__ __forceinline__ bool heard(uint64_t* bar, uint32_t parity, const unsigned* flag, uint64_t limit) {
   if (mbar_try_wait_cluster(bar, parity)) return true;
   const uint64_t t0 = global_timer_ns();
   for (uint32_t it = 1;; ++it) {
     if (mbar_try_wait_cluster(bar, parity)) return true;
-    if ((it & 63u) == 0u && global_timer_ns() - t0 > kWaitLimitNs) return false;
+    if ((it & 63u) == 0u && (any_deaf(flag) || global_timer_ns() - t0 > limit)) return false;
   }
+}
+__device__ __forceinline__ void pause_ns(uint64_t ns) {
+  const uint64_t t0 = global_timer_ns();
+  while (global_timer_ns() - t0 < ns) __nanosleep(1000);
 }
 
 __device__ __forceinline__ float warp_max_nan(float v) {
@@ -309,7 +329,10 @@ __device__ __forceinline__ uint4 shifted(const uint4& a, const uint4& b, int shi
                     __funnelshift_r(w[2], w[3], bits), __funnelshift_r(w[3], w[4], bits));
 }
 
-template <typename T, bool kGrad, TokenEnds kEnds>
+// kLate: the form in which a test has a CTA come late, under a shorter limit.
+constexpr uint64_t kLateLimitNs = 200000000ull;
+
+template <typename T, bool kGrad, TokenEnds kEnds, bool kLate = false>
 __global__ void __launch_bounds__(kGrad ? 128 : 256, kGrad ? 5 : 4)
     token_rows_kernel(const __grid_constant__ TokenParams p, const __grid_constant__ TokenPlan plan) {
   constexpr int kVec = Row<T>::kVec;
@@ -333,6 +356,7 @@ __global__ void __launch_bounds__(kGrad ? 128 : 256, kGrad ? 5 : 4)
     if (tid == 0) {
       mbar_init(&sh.full[0], 1);
       mbar_init(&sh.full[1], 1);
+      sh.deaf = 0;
       fence_mbar_init();
     }
     __syncwarp();
@@ -441,7 +465,7 @@ __global__ void __launch_bounds__(kGrad ? 128 : 256, kGrad ? 5 : 4)
 
   int place = 0;  // of the next batch to work on
   int heard_rows = 0;  // that take part
-  bool deaf = false;   // a wait gave up: no row has a number from there on
+  bool deaf = false;   // (a warp's lanes alike)
 #pragma unroll 1
   for (int turn = 0; turn < turns; ++turn) {
     if (turn - base == 32) {
@@ -497,7 +521,8 @@ __global__ void __launch_bounds__(kGrad ? 128 : 256, kGrad ? 5 : 4)
       if (!kGrad) place = at;
       __syncwarp();
       sum = warp_merged<!kGrad>(sum, c2);
-      if (ctas > 1) {
+      if (ctas > 1 && !deaf) {
+        if (kLate && turn == plan.late_turn && cluster == 0 && rank == ctas - 1) pause_ns(3 * kLateLimitNs);
         if (lane < ctas) tell(&sh.part[buf][rank * warps + warp], &sh.full[buf], lane, sum);
         if (mine)
 #pragma unroll 1
@@ -507,8 +532,10 @@ __global__ void __launch_bounds__(kGrad ? 128 : 256, kGrad ? 5 : 4)
                reinterpret_cast<const float*>(&sh.row[turn & 3])[tid]);
         if (tid == 0) mbar_arrive_expect_tx(&sh.full[buf], ctas * warps * 16 + 4 + (p.policy ? 16 : 0));
         __syncwarp();
-        if (!deaf) deaf = !heard(&sh.full[buf], heard_rows >> 1 & 1);
-      } else {
+        const bool here = heard(&sh.full[buf], heard_rows >> 1 & 1, &sh.deaf, kLate ? kLateLimitNs : kWaitLimitNs);
+        deaf = __any_sync(0xffffffffu, !here || any_deaf(&sh.deaf));
+        if (deaf && lane < ctas) tell_deaf(&sh.deaf, lane);
+      } else if (ctas == 1) {
         if (mine) sh.zt[buf] = zt;
         if (p.policy && tid < 4)
           reinterpret_cast<float*>(&sh.info[buf])[tid] = reinterpret_cast<const float*>(&sh.row[turn & 3])[tid];
@@ -524,7 +551,7 @@ __global__ void __launch_bounds__(kGrad ? 128 : 256, kGrad ? 5 : 4)
       }
       __syncwarp();
       sum = warp_merged<!kGrad>(sum, c2);
-      m = sum.m;
+      m = deaf ? __int_as_float(0x7fc00000) : sum.m;
       s = deaf ? __int_as_float(0x7fc00000) : sum.s + sum.c;
       rest = (sum.s - s) + sum.c;
       zt = sh.zt[buf];
@@ -661,8 +688,11 @@ __global__ void __launch_bounds__(kGrad ? 128 : 256, kGrad ? 5 : 4)
   }
   grid_launch_dependents();
   if (ctas > 1) {
+    // Nothing is on its way into a CTA that leaves: every row's sums were heard of, or what was
+    // told to the deaf, before it was known that they are, has had its time.
+    if (deaf || any_deaf(&sh.deaf)) pause_ns(1000000);
     __syncwarp();
-    cluster_sync();  // nothing is on its way into a CTA that has left
+    cluster_sync();
   }
 }
 

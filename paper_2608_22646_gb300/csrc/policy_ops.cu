@@ -169,7 +169,7 @@ TokenPlan token_plan(int M, int V, bool aligned, const TokenDevice& d) {
       const int c = 1 << ic;
       if (c > 1 && V / c < 1024) break;
       const int n = row_chunk(V, c) / Row<T>::kVec + (aligned ? 0 : 2);
-      TokenPlan plan = {c, s.threads, (n + batch - 1) / batch, most_ring(d.limit, s), 0};
+      TokenPlan plan = {c, s.threads, (n + batch - 1) / batch, most_ring(d.limit, s), 0, -1};
       if (plan.ring > 3 * plan.batches - 1) plan.ring = 3 * plan.batches - 1;
       if (plan.ring > (kGrad ? plan.batches : 0) + 7) plan.ring = (kGrad ? plan.batches : 0) + 7;
       if (kGrad && plan.ring <= plan.batches) continue;
@@ -191,7 +191,7 @@ TokenPlan token_plan(int M, int V, bool aligned, const TokenDevice& d) {
   return best;
 }
 
-template <typename T, bool kGrad, TokenEnds kEnds>
+template <typename T, bool kGrad, TokenEnds kEnds, bool kLate = false>
 int launch_rows(const TokenParams& p, const TokenPlan& plan, void* stream) {
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(static_cast<unsigned>(plan.clusters * plan.ctas));
@@ -202,7 +202,7 @@ int launch_rows(const TokenParams& p, const TokenPlan& plan, void* stream) {
   cluster_of(&cfg, at, plan.ctas);
   after_previous(&cfg, at);
   cudaGetLastError();  // an error left by earlier work is not this call's
-  if (cudaLaunchKernelEx(&cfg, token_rows_kernel<T, kGrad, kEnds>, p, plan) != cudaSuccess) {
+  if (cudaLaunchKernelEx(&cfg, token_rows_kernel<T, kGrad, kEnds, kLate>, p, plan) != cudaSuccess) {
     cudaGetLastError();
     return CAI_ERR_CUDA;
   }
@@ -374,6 +374,36 @@ extern "C" int cai_policy_backward(const void* logits, int32_t dtype, int64_t ld
   p.ld_grad = ld_grad;
   if (M != 0 && !slope) return CAI_ERR_ARG;
   return backward(p, dtype, stream);
+}
+
+extern "C" int cai_test_late_rows(const float* logits, int32_t M, int32_t V, const int32_t* token,
+                                  const float* advantage, int32_t ctas, int32_t late_row, float* loss,
+                                  float* logp, float* stats, float* slope, float* grad, void* stream) {
+  TokenParams p = rows_of(logits, V, M, V, token, 1.0);
+  p.policy = true;
+  p.advantage = advantage;
+  p.low = p.high = 1.0f;
+  p.loss = loss;
+  p.logp = logp;
+  p.stats = stats;
+  p.slope = slope;
+  p.grad = grad;
+  p.ld_grad = V;
+  if (ctas < 2 || ctas > kRowMaxCluster || (ctas & (ctas - 1)) || V < 1024 * ctas || V > 4096 * ctas || V % 4 || M < 1 ||
+      late_row < 0 || late_row >= M)
+    return CAI_ERR_SHAPE;
+  if (!aligned_to(logits, 16) || !aligned_to(grad, 16)) return CAI_ERR_ARG;
+  TokenDevice* d = nullptr;
+  const int r = check(p, CAI_F32, &d);
+  if (r != CAI_OK) return r;
+  if (!token || !advantage || !loss || !logp || !stats || !slope) return CAI_ERR_ARG;
+  // One cluster, so that rows are taken one after another.
+  constexpr int kThreads = 128;
+  TokenPlan plan = {ctas, kThreads, 0, 0, 1, late_row};
+  plan.batches = (row_chunk(V, ctas) / 4 + kThreads * kBatch - 1) / (kThreads * kBatch);
+  plan.ring = plan.batches + 1;
+  return grad ? launch_rows<float, true, kWhole, true>(p, plan, stream)
+              : launch_rows<float, false, kWhole, true>(p, plan, stream);
 }
 
 extern "C" int cai_preference_loss(const float* logp, const float* ref_logp, const float* weight,
