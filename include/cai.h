@@ -599,14 +599,18 @@ int cai_token_logp_backward(const void* logits, int32_t dtype, int64_t ld, int32
  *   loss = weight [ -min(r A, clip(r, 1 - clip_low, 1 + clip_high) A)
  *                   + kl (exp(ref_logp - logp) - (ref_logp - logp) - 1) ],
  * A = advantage, per row; weight NULL: 1; the KL term needs ref_logp where kl is
- * not 0 (ref_logp is not read where it is).  r counts as at most the largest
- * 32-bit number.  With dlogp/dz as above,
+ * not 0 (ref_logp has no effect where it is).  r counts as at most the largest
+ * 32-bit number; it is of logp in 32 bits as it is before its last correction, so that for
+ * the old_logp of the same logits it is 1 to within 4e-6 for a logp of -30.  With dlogp/dz
+ * as above,
  *   d loss / d logp = weight [ -A r, or 0 where r A is above the clipped product,
  *                              + kl (1 - exp(ref_logp - logp)) ].
  * (Without old_logp r is 1 and its derivative that of logp: the plain policy
  * gradient.)  loss, logp [M]; stats [M, 2] as above; slope [M]: d loss / d logp.  A
  * row of weight 0 takes no part, as one without a token.  grad (NULL: none):
  * d loss / d z of every row, as cai_policy_backward gives it for a grad_loss of 1.
+ * (With grad a row's sum is added up more plainly, 1.3e-7 of it and not 6e-8: logp may be
+ * another in its last place than without.)
  * Where a term has no number (a row without a softmax, a token at -inf under the
  * KL term), neither have loss and gradient.  0 <= clip_low <= 1, 0 <= clip_high, all
  * settings finite (else CAI_ERR_ARG).
@@ -629,8 +633,9 @@ int cai_policy_backward(const void* logits, int32_t dtype, int64_t ld, int32_t M
  * Testing hook: cai_policy_loss of dense float32 rows at temperature 1 (without old_logp,
  * ref_logp and weight; grad NULL: none) by one cluster of `ctas` (2, 4 or 8) CTAs, of
  * which one waits 0.6 s before it tells the others its sums of row late_row, while they
- * wait for 0.2 s.  Rows from late_row on that take part are NaN.  No trap and no fault.  1024 ctas <= V <= 4096 ctas,
- * V a multiple of 4, rows on 16-byte boundaries, 0 <= late_row < M.
+ * wait for 0.2 s.  Rows from late_row on that take part are NaN.  No trap and no fault.
+ * 1024 ctas <= V <= 4096 ctas, V a multiple of 4, 0 <= late_row < M (else
+ * CAI_ERR_SHAPE), rows on 16-byte boundaries (else CAI_ERR_ARG).
  */
 int cai_test_late_rows(const float* logits, int32_t M, int32_t V, const int32_t* token,
                        const float* advantage, int32_t ctas, int32_t late_row, float* loss,
@@ -645,7 +650,8 @@ int cai_test_late_rows(const float* logits, int32_t M, int32_t V, const int32_t*
  *   s = sum of weight (logp - ref_logp) over a sequence's rows
  *       (weight NULL: 1, ref_logp NULL: 0; rows of weight 0 are left out),
  *   margin = beta (s_chosen - s_rejected),
- *   loss = -(1 - smoothing) log sigmoid(margin) - smoothing log sigmoid(-margin).
+ *   loss = -(1 - smoothing) log sigmoid(margin) - smoothing log sigmoid(-margin),
+ * a term of the share 0 left out (a suppressed token makes a margin of -inf or +inf).
  * loss, margin: [pairs]; grad_logp [M] (NULL: none): grad_loss [pairs] (NULL: 1)
  * times d loss / d logp, 0 for rows in no sequence: what cai_token_logp_backward
  * takes; no written buffer may overlap another.  M >= 0, 0 <= pairs <= 2^30, beta finite, 0 <= smoothing <= 1.  Errors as

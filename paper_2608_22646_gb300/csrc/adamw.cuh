@@ -56,6 +56,8 @@ struct AdamParams {
   const void* grads[kAdamGroup];
 };
 
+// A mixer of 32 bits that a published search found to be nearly without bias (C. Wellons,
+// "Prospecting for Hash Functions", 2018).
 __device__ __forceinline__ uint32_t adam_mix(uint32_t x) {
   x ^= x >> 16;
   x *= 0x7feb352du;
@@ -419,11 +421,12 @@ struct AdamRun {
 };
 
 // 32-bit states: the bytes bound it, 200 bf16 tensors of 242 M elements 813 us, 96 % of the
-// copy's rate.  8-bit states: 74 instructions an element (a hash of 9, a root of 10, two
+// copy's rate.  8-bit states: 75 instructions an element (a hash of 9, a root of 10, two
 // encodings of 14) and 24 warps an SM cover the loads in part: a head of 518 M float32
-// parameters with bf16 gradients and copies 1445 us, 85 % of the copy's rate.  The next eight
-// elements asked for before the update and not before the encoding: 1484, as
-// registers spill; with 2.7 rounds of CTAs instead of one 1552.
+// parameters with bf16 gradients and copies 1430 us, 86 % of the copy's rate.  (80 registers
+// hold it but for 56 to 60 bytes.)  The next eight elements asked for before the update and not
+// before the encoding: 1484, as more registers spill; with 2.7 rounds of CTAs instead of
+// one 1552.
 //
 // The tensors with parameters of type P: every CTA takes an equal run of all
 // tensors' chunks, one after another.

@@ -147,7 +147,8 @@ bool grad(const NormParams& p, const NormPlan& plan, cudaStream_t s) {
 }
 
 // Rows that lie alike, one for every SM and more: a CTA to an SM, as many units
-// in it as there are rows and threads for.  False: no such rows, or no room for two.
+// in it as there are rows and threads for.  False: no such rows, or no room for two: the
+// ring's places are 512 threads apart whatever the unit, so float32 above 8192 columns has none.
 template <typename T, typename W, int kElems, bool kEdges>
 bool grad_ring(const NormParams& p, int dev, cudaStream_t s) {
   constexpr int kMore = kEdges ? 16 / sizeof(T) - 1 : 0;  // columns in front of a row
@@ -179,7 +180,7 @@ bool grad_rings(const NormParams& p, int dev, cudaStream_t s) {
 template <typename T, typename W, bool kWide>
 bool backward(NormParams& p, int dev, cudaStream_t s) {
   // Rows that start anywhere, an element at a time otherwise: 1000 of 4099 bf16 25 us (64); few
-  // of float32 not: 2000 of 1027 17 us (14), 4000 20 (21).
+  // of float32 not: 2000 of 1027 17 us (14), 4000 20 (21); measured at that width alone.
   const bool edges = !kWide && p.H >= 64 && (sizeof(T) == 2 || p.M >= 32 * kNormSms) && alike(p.x, p.ld, p.gy, p.ld_gy, sizeof(T)) &&
                      (!p.out || alike(p.x, p.ld, p.out, p.ld_out, sizeof(T)));
   if ((kWide || edges) && grad_rings<T, W, !kWide>(p, dev, s)) {

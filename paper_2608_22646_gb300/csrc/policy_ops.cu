@@ -228,7 +228,8 @@ int run_rows(const TokenParams& p, const TokenDevice& d, void* stream) {
   if (p.grad) {
     const TokenPlan plan = token_plan<T, true>(p.M, p.V, aligned, d);
     // bf16 that has to be moved along, with a fifth of a cut's places empty: two kernels, 300
-    // rows of 50003 22 us (25), 600 43 (45); 300 of 126465, a thirtieth empty, 51 (47).
+    // rows of 50003, a quarter empty, 22 us (25), 600 43 (45); 300 of 126465, a thirtieth
+    // empty, 51 (47).  (The border between is not measured.)
     const int vectors = plan.threads ? row_chunk(p.V, plan.ctas) / Row<T>::kVec : 0;
     const bool loose = !alike && sizeof(T) == 2 && plan.clusters < p.M &&
                        5 * vectors < 4 * plan.batches * kBatch * plan.threads;
